@@ -126,7 +126,7 @@ def _quantise(x):
     groups = x.unflatten(-1, (-1, 32))
     most = groups.abs().amax(dim=-1)
     m, e = torch.frexp(most)
-    e = (e - 3 + (m >= 0.875).int()).clamp(-125, 125)
+    e = (e - 3 + (m >= 0.875).int()).clamp(-120, 125)
     y = torch.ldexp(groups.abs(), -e[..., None])
     code = (y > 0.25).to(torch.uint8) + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5)
     code = code + 8 * torch.signbit(groups).to(torch.uint8)
