@@ -186,6 +186,76 @@ int paged_decode_attn_fp8kv(const void* q, const void* k_pool, const void* v_poo
                             void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Pools held in 4 bits, a quarter of the bytes of bf16: values of OCP FP4 E2M1 (a
+ * sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives), and for each group of 32 dims of a token and KV head one scale byte
+ * b that stands for 2^(b - 127) (OCP E8M0; 255 is NaN).  A pool is an array of
+ * tiles of 16 tokens of one KV head, 8.5 * D bytes each, the codes first and then
+ * the scales:
+ *
+ *     [num_pool_blocks][num_kv_heads][block_size / 16] tiles
+ *     codes of a K tile   [D / 32][16 tokens][16 bytes]
+ *     codes of a V tile   [4][D / w][4 tokens][w / 2 bytes], w = 8 dims (4 at
+ *                         D = 64): token t is at [t / 4][.][t % 4]
+ *     scales of a tile    [D / 32][16 tokens]
+ *
+ * the lower dim of two in the lower half of a byte.  A block is 4.25 bits per value
+ * (pkv_fp4_block_bytes: 8704 bytes at 8 x 16 x 128, always a multiple of 32); the
+ * copies (gather, scatter, move, offload, reload) take such a pool as it is, with
+ * that block_bytes.  The paper fixes no quantised format: this one is the library's
+ * choice.
+ */
+int pkv_fp4_block_bytes(const pkv_attn_shape* shape /* host */, size_t* out_bytes);
+
+/*
+ * paged_decode_attn over such pools (q and out bf16, fp32 arithmetic).  Codes and
+ * scale are widened together to bf16, exactly for scale bytes of 7 to 252, the ones
+ * that the appends write, so the result is the attention of the decoded pools to
+ * the same tolerance as the bf16 call.  A NaN scale inside a request's valid rows
+ * acts as NaN in all 32 values; unused slots, whose codes and scales lie in the tile of
+ * used ones, and unused blocks may hold any bytes.
+ *
+ *   k_pool, v_pool  device, 16-byte aligned, tiles as above
+ *   shape           as for paged_decode_attn: every head_dim and block_size
+ */
+int paged_decode_attn_fp4kv(const void* q, const void* k_pool, const void* v_pool,
+                            const int32_t* block_tables, const int32_t* context_lens, float scale,
+                            void* out, const pkv_attn_shape* shape, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * Decode attention of requests that see part of their context: the last `window`
+ * tokens (the one being decoded is one of them) and the first `sinks` ones:
+ *
+ *   out[s,h,:] = sum_t softmax_t( scale * q[s,h,:] . K[s,t,kvh,:] ) * V[s,t,kvh,:]
+ *   for t in [0, L) with t >= L - window or t < sinks,   L = context_lens[s].
+ *
+ * A decode step then reads a bounded part of a cache that grows on.  Everything
+ * else as in paged_decode_attn, paged_decode_attn_fp8kv and paged_decode_attn_fp4kv, with
+ * the same workspace.  A request longer than max_context_len is attended as if it had that
+ * length.  With window >= L or sinks >= L a request sees all of its context.  With window 0
+ * it sees the sinks alone, and with neither its row is all zeros.  Table entries of blocks in which no
+ * token is seen are never read, whatever they hold: such blocks may be freed.
+ * Values of tokens that are not seen never reach the result, NaN included.
+ *
+ *   window, sinks   >= 0 (PKV_ERR_SHAPE otherwise), the same for every request
+ */
+int paged_decode_attn_window(const void* q, const void* k_pool, const void* v_pool,
+                             const int32_t* block_tables, const int32_t* context_lens, float scale,
+                             int32_t window, int32_t sinks, void* out, const pkv_attn_shape* shape,
+                             void* workspace, size_t workspace_bytes, void* stream);
+int paged_decode_attn_window_fp8kv(const void* q, const void* k_pool, const void* v_pool,
+                                   const int32_t* block_tables, const int32_t* context_lens,
+                                   float scale, float k_scale, float v_scale, int32_t window,
+                                   int32_t sinks, void* out, const pkv_attn_shape* shape,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+int paged_decode_attn_window_fp4kv(const void* q, const void* k_pool, const void* v_pool,
+                                   const int32_t* block_tables, const int32_t* context_lens,
+                                   float scale, int32_t window, int32_t sinks, void* out,
+                                   const pkv_attn_shape* shape, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
  * paged_decode_attn for callers that cannot allocate device memory or carry a
  * workspace around: code under HIP graph capture, tight serving loops, harnesses
  * that forbid hipMalloc.  Same arguments, same kernels and bit-identical results,
@@ -325,6 +395,78 @@ int kv_append(const void* k_new, const void* v_new, void* k_pool, void* v_pool,
 int kv_append_fp8(const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                   const int32_t* block_tables, const int32_t* context_lens, float k_scale,
                   float v_scale, const pkv_attn_shape* shape, void* stream);
+
+/*
+ * kv_append for pools held in 4 bits.  The scale of a group of 32 values is the
+ * smallest power of two, between 2^-120 and 2^125, with which none of them is rounded
+ * past 6, and a code is the value nearest to x / scale, ties to the even code, zeros
+ * keeping their sign.  Magnitudes beyond 6 * 2^125, infinity among them, are held there; a
+ * group with a NaN gets the scale byte 255.  Bytes of other tokens are left as they
+ * are.  Everything else as for kv_append.
+ */
+int kv_append_fp4(const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                  const int32_t* block_tables, const int32_t* context_lens,
+                  const pkv_attn_shape* shape, void* stream);
+
+/* The new tokens of one kv_rope_append call and how their rows are turned. */
+typedef struct {
+  int64_t num_tokens;    /* T: rows of q, k, v and q_out, 0..2^24-1                             */
+  int64_t q_stride;      /* elements from a token's row to the next one's, multiples of 8, at   */
+  int64_t k_stride;      /* most 2^31: the rows of one fused projection lie (Hq + 2 Hkv) * D    */
+  int64_t v_stride;      /* apart.  0: rows of Hq * D (Hkv * D) elements without gaps           */
+  int32_t rotary_dim;    /* R: dims that are rotated, a multiple of 16, 0..D; 0: none           */
+  int32_t interleaved;   /* 0: dims j and j + R/2 form a pair; 1: 2j and 2j + 1                 */
+  int32_t num_positions; /* rows of cos_sin; with R > 0 at least max_context_len (MAXB*B if 0)  */
+  float norm_eps;        /* >= 0, finite                                                        */
+} pkv_rope_shape;
+
+/*
+ * New tokens on their way into the cache, from a few decoded ones to whole prompts:
+ * every head's query and key row is normalised and rotated, queries go to q_out, as
+ * attention takes them, keys and values to their slots of the pools.
+ *
+ *   y    = x * rsqrt( mean(x^2) + norm_eps ) * weight          (no weights: y = x)
+ *   out_j = y_j * cos_i - y_p * sin_i,   out_p = y_p * cos_i + y_j * sin_i
+ *
+ * for the R/2 pairs (j, p) of the first R dims, cos_i and sin_i being elements i and
+ * R/2 + i of the row of cos_sin at the token's position; the other dims stay y.
+ * Values are not normalised nor rotated.  fp32 arithmetic, one rounding at the end, to bf16 or
+ * as in kv_append_fp8 and kv_append_fp4.
+ *
+ * Tokens belong to requests in order: request s has tokens token_starts[s] to
+ * token_starts[s+1] - 1, n_s of them, any number of the context_lens[s] it then has, and they are its
+ * last ones: the i-th is at position context_lens[s] - n_s + i.  With token_starts NULL each request has one
+ * (T = num_seqs), as in kv_append.  context_lens[s] is clamped to [0, max_context_len] first.  Tokens without a position
+ * (of requests with fewer context tokens than new ones, before token_starts[0] or from
+ * token_starts[num_seqs] on: padding) are skipped, and their rows of q_out left as they were.  Of a token
+ * whose table entry lies outside [0, num_pool_blocks) only q_out is written.
+ *
+ *   q          device  bf16  T rows of [Hq][D], q_stride apart
+ *   k, v       device  bf16  T rows of [Hkv][D], k_stride and v_stride apart
+ *   q_norm, k_norm  device bf16 [D], the weights; each may be NULL
+ *   cos_sin    device  fp32  [num_positions][R]; may be NULL with R = 0
+ *   q_out      device  bf16  [T][Hq][D]; may be q itself where q has no gaps,
+ *              else it must not overlap the inputs (PKV_ERR_SHAPE where it meets rows of q, k or v)
+ *   k_pool, v_pool, block_tables, context_lens   as for kv_append
+ *   token_starts  device int32 [num_seqs + 1], ascending, or NULL
+ * Pointers to bf16 and fp32 data are 16-byte aligned.  The report of refused ids counts one per token.
+ */
+int kv_rope_append(const void* q, const void* k, const void* v, const void* q_norm,
+                   const void* k_norm, const float* cos_sin, void* q_out, void* k_pool,
+                   void* v_pool, const int32_t* block_tables, const int32_t* context_lens,
+                   const int32_t* token_starts, const pkv_rope_shape* rope /* host */,
+                   const pkv_attn_shape* shape, void* stream);
+int kv_rope_append_fp8(const void* q, const void* k, const void* v, const void* q_norm,
+                       const void* k_norm, const float* cos_sin, void* q_out, void* k_pool,
+                       void* v_pool, const int32_t* block_tables, const int32_t* context_lens,
+                       const int32_t* token_starts, float k_scale, float v_scale,
+                       const pkv_rope_shape* rope /* host */, const pkv_attn_shape* shape,
+                       void* stream);
+int kv_rope_append_fp4(const void* q, const void* k, const void* v, const void* q_norm,
+                       const void* k_norm, const float* cos_sin, void* q_out, void* k_pool,
+                       void* v_pool, const int32_t* block_tables, const int32_t* context_lens,
+                       const int32_t* token_starts, const pkv_rope_shape* rope /* host */,
+                       const pkv_attn_shape* shape, void* stream);
 
 /*
  * Optional report of block ids the kernels refused to follow.  No kernel of this

@@ -30,6 +30,9 @@ EXPORTS = (
     "kv_blocks_gather", "kv_blocks_scatter", "kv_blocks_move", "kv_blocks_offload", "kv_blocks_reload",
     "kv_append", "kv_append_fp8", "pkv_set_id_fault_counter", "pkv_status_string",
     "pkv_last_launch_error", "pkv_version", "pkv_probe_stream_read",
+    "pkv_fp4_block_bytes", "kv_append_fp4", "paged_decode_attn_fp4kv", "paged_decode_attn_window",
+    "paged_decode_attn_window_fp8kv", "paged_decode_attn_window_fp4kv", "kv_rope_append", "kv_rope_append_fp8",
+    "kv_rope_append_fp4",
 )
 
 
@@ -45,6 +48,20 @@ class AttnShape(ctypes.Structure):
         ("partition_size", ctypes.c_int32),
         ("max_context_len", ctypes.c_int32),
         ("num_pool_blocks", ctypes.c_int64),
+    ]
+
+
+class RopeShape(ctypes.Structure):
+    """Mirror of ``pkv_rope_shape``."""
+    _fields_ = [
+        ("num_tokens", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("num_positions", ctypes.c_int32),
+        ("norm_eps", ctypes.c_float),
     ]
 
 
@@ -80,7 +97,7 @@ def _setup_call(L, torch):
         return _ByCtypes()
     addresses = {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS}
     device, stream = (getattr(torch._C, x, None) for x in ("_cuda_getDevice", "_cuda_getCurrentRawStream"))
-    _pkv_call.setup(addresses, AttnShape, torch.cuda.is_initialized, device, stream if device else None)
+    _pkv_call.setup(addresses, AttnShape, RopeShape, torch.cuda.is_initialized, device, stream if device else None)
     return _pkv_call
 
 
@@ -141,6 +158,20 @@ def lib() -> ctypes.CDLL:
         L.kv_append_fp8.restype = ctypes.c_int
         L.kv_append.argtypes = [vp, vp, vp, vp, i32p, i32p, shp, vp]
         L.kv_append.restype = ctypes.c_int
+        f32, i32, rope, size = ctypes.c_float, ctypes.c_int32, ctypes.POINTER(RopeShape), ctypes.c_size_t
+        attn, rows = [vp, vp, vp, i32p, i32p, f32], [vp] * 9 + [i32p] * 3
+        for name, args in (
+                ("pkv_fp4_block_bytes", [shp, ctypes.POINTER(size)]),
+                ("kv_append_fp4", [vp, vp, vp, vp, i32p, i32p, shp, vp]),
+                ("paged_decode_attn_fp4kv", attn + [vp, shp, vp, size, vp]),
+                ("paged_decode_attn_window", attn + [i32, i32, vp, shp, vp, size, vp]),
+                ("paged_decode_attn_window_fp8kv", attn + [f32, f32, i32, i32, vp, shp, vp, size, vp]),
+                ("paged_decode_attn_window_fp4kv", attn + [i32, i32, vp, shp, vp, size, vp]),
+                ("kv_rope_append", rows + [rope, shp, vp]),
+                ("kv_rope_append_fp8", rows + [f32, f32, rope, shp, vp]),
+                ("kv_rope_append_fp4", rows + [rope, shp, vp])):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = ctypes.c_int
         _raw_stream = _find_raw_stream(torch)
         _call = _setup_call(L, torch)
         _lib = L
@@ -210,6 +241,19 @@ def pkv_attn_workspace_bytes(shape: AttnShape) -> int:
     return int(n.value)
 
 
+def pkv_fp4_block_bytes(shape: AttnShape) -> int:
+    """Bytes of a block of a pool held in 4 bits: the size of its images in the copies."""
+    n = ctypes.c_size_t(0)
+    _check(lib().pkv_fp4_block_bytes(ctypes.byref(shape), ctypes.byref(n)))
+    return int(n.value)
+
+
+def make_rope(num_tokens, rotary_dim, num_positions, interleaved=False, norm_eps=1e-6, q_stride=0, k_stride=0,
+              v_stride=0) -> RopeShape:
+    """``num_positions``: rows of the table of cosines and sines; strides are in elements, 0 for rows without gaps."""
+    return RopeShape(num_tokens, q_stride, k_stride, v_stride, rotary_dim, int(interleaved), num_positions, norm_eps)
+
+
 def paged_decode_attn(q, k_pool, v_pool, block_tables, context_lens, scale, out,
                       shape: AttnShape, workspace=None, stream=None) -> None:
     """Enqueue one batched decode-attention call; see ``include/pkv.h``."""
@@ -235,6 +279,64 @@ def paged_decode_attn_fp8kv(q, k_pool, v_pool, block_tables, context_lens, scale
                                                _ptr(context_lens), ctypes.c_float(scale), ctypes.c_float(k_scale),
                                                ctypes.c_float(v_scale), _ptr(out), ctypes.byref(shape),
                                                _ptr(workspace), ws_bytes, _stream(stream))
+    if status:
+        _check(status)
+
+
+def _ws_bytes(workspace) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def paged_decode_attn_fp4kv(q, k_pool, v_pool, block_tables, context_lens, scale, out, shape: AttnShape,
+                            workspace=None, stream=None) -> None:
+    """Attention over pools held in 4 bits (``pkv_fp4_block_bytes`` says how large their blocks are)."""
+    status = (_call or _native()).paged_decode_attn_fp4kv(q, k_pool, v_pool, block_tables, context_lens, scale, out, shape,
+                                                          workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_decode_attn_fp4kv(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(context_lens),
+                                               ctypes.c_float(scale), _ptr(out), ctypes.byref(shape), _ptr(workspace),
+                                               _ws_bytes(workspace), _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_decode_attn_window(q, k_pool, v_pool, block_tables, context_lens, scale, window: int, sinks: int, out,
+                             shape: AttnShape, workspace=None, stream=None) -> None:
+    """Attention of each request over its last ``window`` and first ``sinks`` tokens."""
+    status = (_call or _native()).paged_decode_attn_window(q, k_pool, v_pool, block_tables, context_lens, scale, window, sinks,
+                                                           out, shape, workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_decode_attn_window(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(context_lens),
+                                                ctypes.c_float(scale), window, sinks, _ptr(out), ctypes.byref(shape),
+                                                _ptr(workspace), _ws_bytes(workspace), _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_decode_attn_window_fp8kv(q, k_pool, v_pool, block_tables, context_lens, scale, k_scale, v_scale, window: int,
+                                   sinks: int, out, shape: AttnShape, workspace=None, stream=None) -> None:
+    """The same over e4m3 pools."""
+    status = (_call or _native()).paged_decode_attn_window_fp8kv(q, k_pool, v_pool, block_tables, context_lens, scale, k_scale,
+                                                                 v_scale, window, sinks, out, shape, workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_decode_attn_window_fp8kv(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
+                                                      _ptr(context_lens), ctypes.c_float(scale), ctypes.c_float(k_scale),
+                                                      ctypes.c_float(v_scale), window, sinks, _ptr(out), ctypes.byref(shape),
+                                                      _ptr(workspace), _ws_bytes(workspace), _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_decode_attn_window_fp4kv(q, k_pool, v_pool, block_tables, context_lens, scale, window: int, sinks: int, out,
+                                   shape: AttnShape, workspace=None, stream=None) -> None:
+    """The same over pools held in 4 bits."""
+    status = (_call or _native()).paged_decode_attn_window_fp4kv(q, k_pool, v_pool, block_tables, context_lens, scale, window,
+                                                                 sinks, out, shape, workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_decode_attn_window_fp4kv(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
+                                                      _ptr(context_lens), ctypes.c_float(scale), window, sinks, _ptr(out),
+                                                      ctypes.byref(shape), _ptr(workspace), _ws_bytes(workspace),
+                                                      _stream(stream))
     if status:
         _check(status)
 
@@ -354,5 +456,53 @@ def kv_append_fp8(k_new, v_new, k_pool, v_pool, block_tables, context_lens, k_sc
         status = lib().kv_append_fp8(_ptr(k_new), _ptr(v_new), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
                                      _ptr(context_lens), ctypes.c_float(k_scale), ctypes.c_float(v_scale),
                                      ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def kv_append_fp4(k_new, v_new, k_pool, v_pool, block_tables, context_lens, shape: AttnShape, stream=None) -> None:
+    """Quantise each request's newest K and V rows to 4 bits and write them into slot context_lens[s] - 1."""
+    status = (_call or _native()).kv_append_fp4(k_new, v_new, k_pool, v_pool, block_tables, context_lens, shape, stream)
+    if status is NotImplemented:
+        status = lib().kv_append_fp4(_ptr(k_new), _ptr(v_new), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
+                                     _ptr(context_lens), ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def kv_rope_append(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens, token_starts,
+                   rope: RopeShape, shape: AttnShape, stream=None) -> None:
+    """Normalise and rotate the new tokens' queries and keys; queries go to ``q_out``, keys and values into their slots.  ``q``, ``k`` and ``v``
+    may be views of one projection's rows: their strides are ``rope``'s."""
+    status = (_call or _native()).kv_rope_append(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
+                                                 token_starts, rope, shape, stream)
+    if status is NotImplemented:
+        status = lib().kv_rope_append(*map(_ptr, (q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
+                                                  token_starts)), ctypes.byref(rope), ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def kv_rope_append_fp8(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens, token_starts, k_scale,
+                       v_scale, rope: RopeShape, shape: AttnShape, stream=None) -> None:
+    """The same into e4m3 pools."""
+    status = (_call or _native()).kv_rope_append_fp8(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
+                                                     token_starts, k_scale, v_scale, rope, shape, stream)
+    if status is NotImplemented:
+        status = lib().kv_rope_append_fp8(*map(_ptr, (q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
+                                                      token_starts)), ctypes.c_float(k_scale), ctypes.c_float(v_scale),
+                                          ctypes.byref(rope), ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def kv_rope_append_fp4(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens, token_starts,
+                       rope: RopeShape, shape: AttnShape, stream=None) -> None:
+    """The same into pools held in 4 bits."""
+    status = (_call or _native()).kv_rope_append_fp4(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
+                                                     token_starts, rope, shape, stream)
+    if status is NotImplemented:
+        status = lib().kv_rope_append_fp4(*map(_ptr, (q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
+                                                      token_starts)), ctypes.byref(rope), ctypes.byref(shape), _stream(stream))
     if status:
         _check(status)

@@ -79,6 +79,7 @@
 #pragma once
 
 #include "attn_partial.h"
+#include "fp4.h"
 #include "pkv_kernels.h"
 
 #include <type_traits>
@@ -117,6 +118,20 @@ template <> struct Dim<256, true> {
   static constexpr int kKSteps = 8, kKLoads = 4, kVLoads = 8, kTiles = 16, kElemBytes = 1;
   typedef uint32_t VReg __attribute__((ext_vector_type(2)));
 };
+// E2M1 codes with a scale for each 32 dims (tiles, fp4.h), widened to bf16 in registers (exactly, scale and all).  K: a lane has 32 dims of token
+// n, 16 at D = 64; V: the lane's dims of tokens 4*c .. 4*c + 3, in one load (one for each half at D = 256).
+template <int kD> struct Fp4Dim {
+  static constexpr int kKSteps = kD / 32, kKLoads = kD == 256 ? 2 : 1, kVLoads = kKLoads, kTiles = kD / 16, kElemBytes = 1;
+  typedef uint32_t Codes __attribute__((ext_vector_type(kD == 64 ? 2 : 4)));
+  struct Load {
+    Codes codes;
+    uint32_t scales;   // K: the lane's; V: of its four tokens, a byte each
+  };
+  typedef Load VReg;
+};
+// What a wavefront's K load leaves in a lane.
+template <int kD, bool kFp4> struct KLoadOf { typedef u32x4 Type; };
+template <int kD> struct KLoadOf<kD, true> { typedef typename Fp4Dim<kD>::Load Type; };
 // First dim of output tiles 4t..4t+3 (they are consecutive dims) in the lane of column n.
 template <int kD> __device__ __forceinline__ int tile_group_dim(int t, int n) {
   if (kD == 64) return 4 * n;
@@ -142,6 +157,22 @@ __device__ __forceinline__ u32x2 widen_e4m3x4(uint32_t w) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true))};
 }
 
+// The bf16 pairs of a dword of eight codes, times the scale (its exponent counts; 255 gives NaN).
+__device__ __forceinline__ u32x4 widen_e2m1x8(uint32_t w, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Registers that a load may still write to are their own up to here.
+template <typename T>
+__device__ __forceinline__ void arrived(const T& x) {
+  if constexpr (std::is_class_v<T>) asm volatile("" : : "v"(x.codes), "v"(x.scales));
+  else asm volatile("" : : "v"(x));
+}
+
 // Stores of finished rows and of records.  They are written as opaque instructions on
 // purpose: gfx9-family hardware counts loads and stores in one counter, and once
 // the compiler knows a store is pending it can no longer wait for "all but the N
@@ -165,13 +196,14 @@ __device__ __forceinline__ T load_nt(__amdgpu_buffer_rsrc_t b, int offset) {
   constexpr int kNt = 2;
   if constexpr (sizeof(T) == 16) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b128(b, offset, 0, kNt));
   else if constexpr (sizeof(T) == 8) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(b, offset, 0, kNt));
+  else if constexpr (sizeof(T) == 1) return __builtin_amdgcn_raw_buffer_load_b8(b, offset, 0, kNt);
   else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, kNt));
 }
 
 // One window of block descriptors: lane i describes stream index jbase + i.
 struct Window {
   int slab;   // which slab (16 tokens of one KV head; 4 KiB at D = 128 in bf16), counted from the pool's start; 0 when not read
-  int meta;   // bits 0-7 valid tokens (0..16), then the kMeta flags
+  int meta;   // bits 0-7 valid tokens (0..16), then the kMeta flags; with a span, bits 16-31 the tokens that are seen
   int seg;    // s * Hkv + kvh: the segment, whose first query/output row is seg * G
 };
 // A position of the stream: block b of the nb blocks of request s, KV head kvh.
@@ -219,17 +251,21 @@ __device__ __forceinline__ const AttnLaunch& reread(const AttnLaunch&) {
 // kLarge: as large batches want it (large_at_256; at D = 128 in bf16 all but short ones, short_at_128).
 template <int kD, bool kFp8, typename Layers, bool kLarge>
 __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnLaunch a, Layers layers) {
-  typedef Dim<kD, kFp8> DD;
-  typedef typename DD::VReg VReg;                 // one V load as it arrives
+  constexpr bool kFp4 = std::is_base_of_v<Fp4Pools, Layers>;   // kFp8 is set with it: pools that are widened
+  constexpr bool kSpan = std::is_base_of_v<SpanLayer, Layers>;
+  typedef std::conditional_t<kFp4, Fp4Dim<kD>, Dim<kD, kFp8>> DD;
+  typedef typename KLoadOf<kD, kFp4>::Type KReg;  // one K load as it arrives
+  typedef typename DD::VReg VReg;                 // one V load
   typedef typename Dim<kD, false>::VReg VOp;      // the same rows as bf16
   constexpr int kKSteps = DD::kKSteps, kKLoads = DD::kKLoads, kVLoads = DD::kVLoads,
                 kTiles = DD::kTiles, kElemBytes = DD::kElemBytes;
   // V goes out when K is there, not a block ahead, and with it some of the next block's K loads: kAhead, or all where shares are
   // short (short_at_128; AttnLayers have a workgroup for each short segment).
   constexpr bool kLate = !kFp8 && (kD == 128 || (kD == 256 && kLarge));
-  constexpr bool kWhole = std::is_same_v<Layers, WholeLayer>;
+  constexpr bool kWhole = std::is_base_of_v<WholeLayer, Layers>;
   constexpr int kNextK = kD == 128 && (!kLarge || std::is_same_v<Layers, AttnLayers>) ? kKLoads : kAhead;
-  constexpr bool kTwoBlocks = kD == 64 && kFp8;   // the next block's loads go out before this one's have arrived
+  // the next block's loads go out before this one's have arrived
+  constexpr bool kTwoBlocks = kFp4 ? kD <= 128 : kD == 64 && kFp8;
   constexpr int kGroupWaves = group_waves(kD), kThreads = kGroupWaves * 64;
   extern __shared__ __align__(16) int smem[];
   int* cumB = smem;                  // [S+1] blocks before request s
@@ -270,7 +306,14 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     for (int jj = 0; jj < kKSteps; ++jj)
       // dims of step jj in this lane: 32*jj + 8*c .. +7, or, following the byte order of an
       // e4m3 K load, 64*(jj/2) + 16*c + 8*(jj%2) .. +7
-      qnext[jj] = kFp8 ? qrow_p[8 * (jj >> 1) + 2 * c + (jj & 1)] : qrow_p[4 * jj + c];
+      // (E2M1: the order of a lane's codes, 16 or 32 dims of a group)
+      qnext[jj] = kFp4 ? qrow_p[kD == 64 ? 2 * c + jj : 16 * (jj >> 2) + 4 * c + (jj & 3)]
+                  : kFp8 ? qrow_p[8 * (jj >> 1) + 2 * c + (jj & 1)] : qrow_p[4 * jj + c];
+  };
+  // Units of a request of L tokens that are attended over.
+  auto units_of = [&](int L) -> int {
+    if constexpr (kSpan) return layers.span.units(L);
+    else return (L + kBlockTokens - 1) / kBlockTokens;
   };
   if constexpr (!kWhole) {
     // Prefix sums over the requests.  Up to 64: every wavefront for itself, all to the same place and the same values, so that none
@@ -285,7 +328,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     for (int base = S > 64 ? 64 * wave : 0; base < S; base += kThreads) {
       const int i = base + lane;
       const int L = (i < S) ? min(max(a.context_lens[i], 0), a.max_ctx) : 0;
-      const int nb = (L + kBlockTokens - 1) / kBlockTokens;
+      const int nb = units_of(L);
       longest = max(longest, nb);
       const int xb = wave_prefix(nb);
       if (i < S) { lens[i] = L; cumB[i] = xb - nb; }
@@ -406,7 +449,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   auto the_request = [&](int s) -> Request {   // the same for all lanes
     if (S > 64) return request(s);
     const int len = __builtin_amdgcn_readlane(own_len, s);
-    return Request{__builtin_amdgcn_readlane(own_start, s), (len + kBlockTokens - 1) / kBlockTokens, len};
+    return Request{__builtin_amdgcn_readlane(own_start, s), units_of(len), len};
   };
   auto place = [&](int pos, int s, const Request& r) -> Place {
     // o / nb, which is less than Hkv (at most kMaxHeads): the estimate is off by less than one
@@ -439,20 +482,23 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     }
     const Place at = place(pos, s, r);
     const int kvh = at.kvh, b = at.b, nb = at.nb;
-    int ntok = min(kBlockTokens, r.len - kBlockTokens * b);
-    // unit b of the request lies in physical block b / upb, at unit b % upb of the KV head's rows
-    const int tb = b >> upb_bits;
+    int u = b;   // unit of the request
+    if constexpr (kSpan) u = layers.span.unit(b, r.len);
+    int ntok = min(kBlockTokens, r.len - kBlockTokens * u);
+    // unit u of the request lies in physical block u / upb, at unit u % upb of the KV head's rows
+    const int tb = u >> upb_bits;
     const int id = live ? a.block_tables[(int64_t)s * a.MAXB + tb] : -1;
     const bool mapped = (unsigned)id < (unsigned)a.NB;   // ids outside the pool are never followed
     if (!mapped) ntok = 0;
     refused += __popcll(__ballot(live && !mapped));
     Window d;
-    d.slab = mapped ? ((id * Hkv + kvh) << upb_bits) + (b - (tb << upb_bits)) : 0;
+    d.slab = mapped ? ((id * Hkv + kvh) << upb_bits) + (u - (tb << upb_bits)) : 0;
     bool last = (b + 1 == nb) || (j + 1 == nshare);
     if (__any(nb > bpp)) last |= (unsigned)(b + 1) % (unsigned)bpp == 0;
     const bool seg_first = (b == 0) || (j == 0);
     d.meta = ntok | (last ? kMetaLast : 0) | (seg_first ? kMetaSegFirst : 0) |
              (b + 1 == nb ? kMetaSegEnd : 0) | (b > j ? kMetaOpenLeft : 0);
+    if constexpr (kSpan) d.meta |= (int)((mapped ? layers.span.seen(u, r.len) : 0u) << 16);
     if (!live) d.meta = 0;
     d.seg = s * Hkv + kvh;
     return d;
@@ -481,13 +527,13 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   Window dB = {0, 0, 0};   // described when the first blocks have been consumed (below)
   int jbase = 0;           // stream index of window A's first block
 
-  const int64_t slab_bytes = (int64_t)kBlockTokens * kD * kElemBytes;  // one (block, KV head) slab
+  const int64_t slab_bytes = kFp4 ? fp4_tile_bytes(kD) : (int64_t)kBlockTokens * kD * kElemBytes;  // one (block, KV head) slab
   const int tau = turn_token(n);
   // K, in 16-byte pieces of the slab: a wavefront's load is 64 of them in a row, turned in LDS (turn_place).  Straight in
   // operand order, 4 of each token, where that is all of a token's (e4m3 at D = 64), where LDS has no room (stream_lds), and in
   // large batches in e4m3 at D = 256.
   constexpr int kPieces = kD * kElemBytes / 16;   // of a token
-  const bool turns = kD == 128 ? a.turns : !kFp8 || (kD == 256 && !kLarge);
+  const bool turns = !kFp4 && (kD == 128 ? a.turns : !kFp8 || (kD == 256 && !kLarge));
   const int koff = turns ? lane : tau * kPieces + c;
   u32x4* turn = (u32x4*)(wave_lds + kGroupWaves * a.wave_lds_floats) + wave * (kBlockTokens * kPieces);
   // V, in units of one VReg: token 4*e + c, this lane's dims (of half h when D = 256)
@@ -515,11 +561,19 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   // 16..512 tokens 109.5 -> 106.0 us, shares of 1 to 4 blocks at D = 128 0.98 of the time, 72 shapes of 8-bit pools at D = 64 0.983.
   auto rows_of = [&](const void* pool, Block at) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)pool + at.slab * slab_bytes), 0,
-                                             (at.meta & 0xff) * (kD * kElemBytes), kRawBuffer);
+                                             kFp4 ? ((at.meta & 0xff) ? fp4_tile_bytes(kD) : 0) : (at.meta & 0xff) * (kD * kElemBytes),
+                                             kRawBuffer);
   };
-  auto issue_k = [&](u32x4 (&k)[kKLoads], Block at, int from, int to) {
+  auto issue_k = [&](KReg (&k)[kKLoads], Block at, int from, int to) {
     const __amdgpu_buffer_rsrc_t b = rows_of(layer.k_pool, at);
-    if (turns) {
+    if constexpr (kFp4) {
+      typedef typename DD::Codes Codes;
+#pragma unroll
+      for (int jj = from; jj < to; ++jj) {
+        k[jj].codes = load_nt<Codes>(b, kD == 64 ? 256 * (c >> 1) + 16 * n + 8 * (c & 1) : 16 * (64 * jj + lane));
+        k[jj].scales = load_nt<uint8_t>(b, 8 * kD + (kD == 64 ? 16 * (c >> 1) + n : 64 * jj + lane));
+      }
+    } else if (turns) {
 #pragma unroll
       for (int jj = from; jj < to; ++jj) k[jj] = load_nt<u32x4>(b, 16 * (koff + 64 * jj));
     } else {
@@ -530,7 +584,14 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   auto issue_v = [&](VReg (&v)[kVLoads], Block at) {
     const __amdgpu_buffer_rsrc_t b = rows_of(layer.v_pool, at);
     constexpr int kBytes = sizeof(VReg);
-    if (kD == 256) {
+    if constexpr (kFp4) {
+      typedef typename DD::Codes Codes;
+#pragma unroll
+      for (int h = 0; h < kVLoads; ++h) {
+        v[h].codes = load_nt<Codes>(b, (int)sizeof(Codes) * (kD == 256 ? 32 * c + 16 * h + n : lane));
+        v[h].scales = load_nt<uint32_t>(b, 8 * kD + 16 * (kD == 64 ? n >> 3 : 4 * h + (n >> 2)) + 4 * c);
+      }
+    } else if constexpr (kD == 256) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         v[2 * e] = load_nt<VReg>(b, kBytes * (voff + 128 * e));
@@ -542,8 +603,9 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     }
   };
   // K of a block that has arrived, into LDS and back as the A operand: load L of lane (n, c) is piece 4L + c of token tau(n).
-  auto turn_k = [&](u32x4 (&k)[kKLoads]) {
-    if (turns) {
+  auto turn_k = [&](KReg (&k)[kKLoads]) {
+    if constexpr (kFp4) return;
+    else if (turns) {
 #pragma unroll
       for (int jj = 0; jj < kKLoads; ++jj) {
         const int at = 64 * jj + lane;
@@ -573,17 +635,22 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     nstaged = 0;
   };
 
-  auto consume = [&](u32x4 (&kraw)[kKLoads], VReg (&vraw)[kVLoads], int meta) __attribute__((always_inline)) {
+  auto consume = [&](KReg (&kraw)[kKLoads], VReg (&vraw)[kVLoads], int meta) __attribute__((always_inline)) {
     // The MFMA operands.  bf16 pools: the registers as they are.  e4m3 pools: piece 4L + c of
     // K's row holds dims 16*(4L + c) .. +15 of token tau(n), which feed steps 2L and 2L + 1 (the
     // contraction order is free as long as q follows it, see below); a V load holds the same
     // token and dims as in a bf16 pool, one byte each.
     u32x4 k[kKSteps];
-    VOp v[kVLoads];
+    constexpr int kVRows = kD == 256 ? 8 : 4;
+    VOp v[kVRows];
 #pragma unroll
     for (int jj = 0; jj < kKLoads; ++jj) {
-      const u32x4 x = kraw[jj];
-      if constexpr (kFp8) {
+      const auto x = kraw[jj];
+      if constexpr (kFp4) {
+        constexpr int kPer = kKSteps / kKLoads;
+#pragma unroll
+        for (int w = 0; w < kPer; ++w) k[kPer * jj + w] = widen_e2m1x8(x.codes[w], scale_of(x.scales));
+      } else if constexpr (kFp8) {
         const u32x2 y[4] = {widen_e4m3x4(x.x), widen_e4m3x4(x.y), widen_e4m3x4(x.z), widen_e4m3x4(x.w)};
         k[2 * jj] = u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
         k[2 * jj + 1] = u32x4{y[2].x, y[2].y, y[3].x, y[3].y};
@@ -592,8 +659,19 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       }
     }
 #pragma unroll
-    for (int e = 0; e < kVLoads; ++e) {
-      if constexpr (!kFp8) {
+    for (int e = 0; e < kVRows; ++e) {
+      if constexpr (kFp4) {
+        // token 4*c + t, in half h at D = 256
+        const int t = kD == 256 ? e >> 1 : e, h = kD == 256 ? e & 1 : 0;
+        const float scale = scale_of((vraw[h].scales >> (8 * t)) & 0xff);
+        if constexpr (kD == 64) {
+          const uint32_t w = vraw[0].codes[t >> 1] >> (16 * (t & 1));
+          v[e] = VOp{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1))};
+        } else {
+          v[e] = widen_e2m1x8(vraw[h].codes[t], scale);
+        }
+      } else if constexpr (!kFp8) {
         v[e] = vraw[e];
       } else if constexpr (kD == 64) {
         v[e] = widen_e4m3x4(vraw[e]);
@@ -603,6 +681,9 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       }
     }
     const int ntok = meta & 0xff;
+    const uint32_t seen = (uint32_t)meta >> 16;   // with a span
+    // element e of a lane's scores and weights is this token
+    auto token = [&](int e) { return kFp4 ? 4 * c + e : 4 * e + c; };
 
     f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -611,15 +692,21 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
                                                    __builtin_bit_cast(bf16x8, qop[jj]), sc, 0, 0, 0);
     float x[4] = {sc.x * a.scale_log2e, sc.y * a.scale_log2e, sc.z * a.scale_log2e,
                   sc.w * a.scale_log2e};
-    const bool edge = ntok < kBlockTokens;
+    const bool edge = kSpan ? seen != 0xffff : ntok < kBlockTokens;
     bool valid[4] = {true, true, true, true};
     if (edge) {
       // Last block of a request, or an unmapped one: the rows behind it are zeros, and their
-      // scores and weights are replaced by select.  Element e of this lane is token 4*e + c.
+      // scores and weights are replaced by select.
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        valid[e] = 4 * e + c < ntok;
+        valid[e] = kSpan ? (seen >> token(e)) & 1 : token(e) < ntok;
         x[e] = valid[e] ? x[e] : kNegInf;
+      }
+      if constexpr (kSpan || kFp4) {
+        // Rows that are there but not seen, a tile's unused ones: a weight of zero does not silence a NaN in V.
+        constexpr int st = kD == 256 ? 2 : 1;
+#pragma unroll
+        for (int e = 0; e < kVRows; ++e) v[e] = valid[e / st] ? v[e] : VOp{};
       }
     }
     const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
@@ -760,13 +847,13 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     for (int jj = 0; jj < kKSteps; ++jj) qop[jj] = (n < G) ? qnext[jj] : u32x4{0, 0, 0, 0};
   };
   // Waits for loads where it is known how many are younger.
-  auto arrived_k = [](u32x4 (&k)[kKLoads]) {
+  auto arrived_k = [](KReg (&k)[kKLoads]) {
 #pragma unroll
-    for (int jj = 0; jj < kKLoads; ++jj) asm volatile("" : : "v"(k[jj]));
+    for (int jj = 0; jj < kKLoads; ++jj) arrived(k[jj]);
   };
   auto arrived_v = [](VReg (&v)[kVLoads]) {
 #pragma unroll
-    for (int e = 0; e < kVLoads; ++e) asm volatile("" : : "v"(v[e]));
+    for (int e = 0; e < kVLoads; ++e) arrived(v[e]);
   };
   auto ask_q = [&](VReg (&v)[kVLoads], int j, int meta) {   // v: of the block before
     if (kWhole || !(meta & kMetaSegFirst)) return;
@@ -774,7 +861,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     load_q(__builtin_amdgcn_readlane(dA.seg, j - jbase));
   };
 
-  u32x4 kbuf[2][kKLoads];   // two blocks in turn, so that no buffer is ever copied
+  KReg kbuf[2][kKLoads];   // two blocks in turn, so that no buffer is ever copied
   VReg vbuf[2][kVLoads];
   Block at = block_at(0);
   issue_k(kbuf[0], at, 0, kKLoads);
@@ -797,7 +884,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   for (int j = 0; j < nshare; j += 2) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      u32x4 (&k)[kKLoads] = kbuf[i], (&knext)[kKLoads] = kbuf[i ^ 1];
+      KReg (&k)[kKLoads] = kbuf[i], (&knext)[kKLoads] = kbuf[i ^ 1];
       VReg (&v)[kVLoads] = vbuf[i], (&vnext)[kVLoads] = vbuf[i ^ 1];
       if (!kTwoBlocks) arrived_k(k);
       if (!kTwoBlocks && !kLate) arrived_v(v);
@@ -838,9 +925,9 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
 #pragma unroll
     for (int jj = 0; jj < kKSteps; ++jj) asm volatile("" : : "v"(qnext[jj]));
 #pragma unroll
-    for (int jj = 0; jj < kKLoads; ++jj) asm volatile("" : : "v"(kbuf[0][jj]));
+    for (int jj = 0; jj < kKLoads; ++jj) arrived(kbuf[0][jj]);
 #pragma unroll
-    for (int e = 0; e < kVLoads; ++e) asm volatile("" : : "v"(vbuf[kLate][e]));
+    for (int e = 0; e < kVLoads; ++e) arrived(vbuf[kLate][e]);
   }
   // Refused ids are reported once per wavefront, after the stream: nothing in the loop waits on it.
   if (a.id_faults && refused && lane == 0) atomicAdd(a.id_faults, refused);

@@ -1,8 +1,5 @@
-// C-ABI layer of libpkv: argument validation (all of it before any launch, so
-// it can be exercised without a GPU), launch geometry, status codes.
-#include "../../include/pkv.h"
-
-#include "pkv_kernels.h"
+// C-ABI layer of libpkv: attention, append and the copies (pkv_host.h has what the entry points share).
+#include "pkv_host.h"
 
 #include <atomic>
 
@@ -13,81 +10,9 @@
 constexpr size_t kStaticScratchBytes = PKV_STATIC_WORKSPACE_BYTES;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
+using namespace pkv;
+
 namespace {
-
-thread_local hipError_t g_last_launch_error = hipSuccess;
-thread_local int32_t* g_id_faults = nullptr;   // see pkv_set_id_fault_counter
-
-inline bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-// Library's partition choice when the caller leaves it open.  With the stream
-// decomposition a partition only bounds how many tokens one partial result may
-// stand for before it is folded into its segment's record, so the largest value
-// is the cheapest.
-constexpr int kDefaultPartition = pkv::kMaxPartition;
-
-// Query heads.  Keeps every size product far inside 64 bits.
-constexpr int kMaxHeads = 16384;
-
-struct Geometry {
-  int G, P, max_ctx;
-  int64_t slots;   // records that the workspace has room for
-};
-
-// A record for every (wavefront, request, KV head) that meet, at most, as wavefronts' own records would need.  Workgroups leave far
-// fewer; the rest takes those of further layers of a launch, or rows (launch_layer).
-int64_t record_slots(int S, int Hkv) { return (int64_t)Hkv * S + pkv::kStreamWaves; }
-
-int check_shape(const pkv_attn_shape* sh, Geometry* g) {
-  if (!sh) return PKV_ERR_NULL;
-  if (sh->num_seqs < 0 || sh->num_seqs > pkv::kMaxSeqs) return PKV_ERR_SHAPE;
-  if (sh->num_q_heads <= 0 || sh->num_kv_heads <= 0 || sh->num_q_heads > kMaxHeads)
-    return PKV_ERR_SHAPE;
-  const int D = sh->head_dim;
-  if (D != 64 && D != 128 && D != 256) return PKV_ERR_SHAPE;
-  const int B = sh->block_size;
-  if (B != 16 && B != 32 && B != pkv::kMaxBlockSize) return PKV_ERR_SHAPE;
-  if (sh->num_q_heads % sh->num_kv_heads != 0) return PKV_ERR_SHAPE;
-  const int G = sh->num_q_heads / sh->num_kv_heads;
-  if (G > pkv::kMaxGroup) return PKV_ERR_SHAPE;
-  // a wavefront keeps two whole records (G rows of D floats) in its share of LDS
-  if (D == 256 && G > 8) return PKV_ERR_SHAPE;
-  if (sh->max_blocks_per_seq <= 0) return PKV_ERR_SHAPE;
-  if ((int64_t)sh->max_blocks_per_seq * B > INT32_MAX) return PKV_ERR_SHAPE;
-  const int cap = sh->max_blocks_per_seq * B;
-  if (sh->max_context_len < 0 || sh->max_context_len > cap) return PKV_ERR_SHAPE;
-  const int max_ctx = sh->max_context_len ? sh->max_context_len : cap;
-  int P = sh->partition_size;
-  if (P < 0) return PKV_ERR_SHAPE;
-  if (P == 0) P = kDefaultPartition;
-  if (P % B != 0 || P < B || P > pkv::kMaxPartition) return PKV_ERR_SHAPE;
-  // 4 KiB slabs (16 tokens of one KV head) are numbered in 32 bits on the device
-  if (sh->num_pool_blocks < 1 ||
-      sh->num_pool_blocks > INT32_MAX / ((int64_t)sh->num_kv_heads * (B / pkv::kBlockTokens)))
-    return PKV_ERR_SHAPE;
-  // stream positions, slots and rows are 32-bit on the device
-  const int64_t max_blocks = (max_ctx + pkv::kBlockTokens - 1) / pkv::kBlockTokens;
-  if ((int64_t)sh->num_kv_heads * sh->num_seqs * max_blocks > INT32_MAX) return PKV_ERR_SHAPE;
-  if ((int64_t)sh->num_seqs * sh->num_q_heads > INT32_MAX) return PKV_ERR_SHAPE;
-  g->G = G;
-  g->P = P;
-  g->max_ctx = max_ctx;
-  g->slots = record_slots(sh->num_seqs, sh->num_kv_heads);
-  return PKV_OK;
-}
-
-// Workspace: the partial records, then room for a prefix array, which nothing uses but which is part of the size that callers know.
-size_t workspace_bytes(const pkv_attn_shape* sh, const Geometry& g) {
-  if (sh->num_seqs == 0) return 0;
-  const size_t records = (size_t)g.slots * pkv::record_floats(g.G, sh->head_dim) * sizeof(float);
-  return records + (((size_t)(sh->num_seqs + 1) * sizeof(int32_t) + 15) & ~(size_t)15);
-}
-
-int launch_status(hipError_t e) {
-  if (e == hipSuccess) return PKV_OK;
-  g_last_launch_error = e;
-  return PKV_ERR_LAUNCH;
-}
 
 // Every GPU holds its own copy of `scratch` at its own address; the address is
 // looked up once per device, with that device current, and kept.
@@ -114,7 +39,7 @@ int static_scratch(void** out) {
 
 extern "C" {
 
-int pkv_version(void) { return 1003; }
+int pkv_version(void) { return 1004; }
 
 const char* pkv_status_string(int status) {
   switch (status) {
@@ -165,125 +90,18 @@ int pkv_attn_workspace_bytes(const pkv_attn_shape* shape, size_t* out_bytes) {
   return PKV_OK;
 }
 
-// Validation shared by the single-layer and the multi-layer call; fills the
-// launch descriptor except for the per-layer pointers.
-static int prepare_attn(const int32_t* block_tables, const int32_t* context_lens, float scale, bool kv_fp8,
-                        const pkv_attn_shape* shape, void* workspace, size_t workspace_bytes_given,
-                        pkv::AttnLaunch* a, bool* empty) {
-  Geometry g;
-  const int rc = check_shape(shape, &g);
-  if (rc != PKV_OK) return rc;
-  *empty = shape->num_seqs == 0;
-  if (*empty) return PKV_OK;
-  if (!block_tables || !context_lens) return PKV_ERR_NULL;
-  if ((reinterpret_cast<uintptr_t>(block_tables) & 3u) || (reinterpret_cast<uintptr_t>(context_lens) & 3u))
-    return PKV_ERR_ALIGN;
-  const size_t need = workspace_bytes(shape, g);
-  if (need) {
-    if (!workspace || workspace_bytes_given < need) return PKV_ERR_WORKSPACE;
-    if (misaligned16(workspace)) return PKV_ERR_ALIGN;
-  }
-  a->block_tables = block_tables;
-  a->context_lens = context_lens;
-  a->S = shape->num_seqs;
-  a->Hq = shape->num_q_heads;
-  a->Hkv = shape->num_kv_heads;
-  a->G = g.G;
-  a->D = shape->head_dim;
-  a->waves = pkv::kLayerGroups * pkv::group_waves(shape->head_dim);
-  const int group = pkv::group_waves(shape->head_dim);
-  const int64_t segments = (int64_t)a->S * a->Hkv;
-  const int64_t max_blocks = (g.max_ctx + pkv::kBlockTokens - 1) / pkv::kBlockTokens;
-  a->short_blocks = pkv::short_segment(segments, a->D, kv_fp8);
-  a->leaves_records = 1;
-  if (segments <= a->waves / group && max_blocks <= a->short_blocks) {
-    // Cut along its segments, a workgroup for each.  Nothing is left in the workspace, and the layers of such
-    // a launch may be more than it has room for.
-    a->leaves_records = 0;
-    a->waves = (int)segments * group;
-  }
-  a->id_faults = g_id_faults;
-  a->MAXB = shape->max_blocks_per_seq;
-  a->upb = shape->block_size / pkv::kBlockTokens;
-  a->P = g.P;
-  a->max_ctx = g.max_ctx;
-  a->NB = (int)shape->num_pool_blocks;
-  a->scale_log2e = scale * 1.4426950408889634f;
-  a->out_scale = 1.f;
-  a->kv_fp8 = kv_fp8;
-  a->ws_rec = static_cast<float*>(workspace);
-  a->ws_words = a->ws_rec + (int64_t)pkv::kRecordsBeforeWords * pkv::record_floats(a->G, a->D);
-  a->layer_ws_floats = pkv::layer_ws_floats(g.G, a->D);
-  return PKV_OK;
-}
-
-static int check_layer_pointers(const void* q, const void* k_pool, const void* v_pool, const void* out) {
-  if (!q || !k_pool || !v_pool || !out) return PKV_ERR_NULL;
-  if (misaligned16(q) || misaligned16(k_pool) || misaligned16(v_pool) || misaligned16(out))
-    return PKV_ERR_ALIGN;
-  return PKV_OK;
-}
-
-static pkv::AttnLayer layer_of(const void* q, const void* k_pool, const void* v_pool, void* out) {
-  return pkv::AttnLayer{static_cast<const uint16_t*>(q), k_pool, v_pool, static_cast<uint16_t*>(out)};
-}
-
-// The launches for the layer of `a`, or for `layers`.
-static int launch_attn(const pkv::AttnLaunch& a, const pkv::AttnLayers* layers, hipStream_t st) {
-  hipError_t e = pkv::launch_attn_stream(a, layers, st);
-  if (e == hipSuccess && a.leaves_records) e = pkv::launch_attn_reduce(a, layers, st);
-  if (e != hipSuccess) return launch_status(e);
-  return PKV_OK;
-}
-
-static uint64_t row_bytes(const pkv::AttnLaunch& a) { return (uint64_t)a.S * a.Hq * a.D * 2; }
-
-// Does layer x's output overlap these bytes?
-static bool overlaps(const pkv::AttnLaunch& a, const pkv::AttnLayer& x, const void* p, uint64_t bytes) {
-  const uint64_t out = reinterpret_cast<uintptr_t>(x.out), at = reinterpret_cast<uintptr_t>(p);
-  return out < at + bytes && at < out + row_bytes(a);
-}
-
-static bool overlaps_pools(const pkv::AttnLaunch& a, const pkv::AttnLayer& x, const pkv::AttnLayer& y) {
-  const uint64_t pool = (uint64_t)a.NB * a.Hkv * a.upb * pkv::kBlockTokens * a.D * (a.kv_fp8 ? 1 : 2);
-  return overlaps(a, x, y.k_pool, pool) || overlaps(a, x, y.v_pool, pool);
-}
-
-// Does what layer x writes overlap what layer y reads or writes?  Then they cannot share a launch.
-static bool writes_into(const pkv::AttnLaunch& a, const pkv::AttnLayer& x, const pkv::AttnLayer& y) {
-  return overlaps(a, x, y.q, row_bytes(a)) || overlaps(a, x, y.out, row_bytes(a)) || overlaps_pools(a, x, y);
-}
-
-// Does a layer write into its own inputs?  The stream pass stores rows while others are still being read, which
-// is right where the output is q itself: a segment's rows of q are read by those who write them.
-static bool writes_own_input(const pkv::AttnLaunch& a, const pkv::AttnLayer& x) {
-  return (x.out != x.q && overlaps(a, x, x.q, row_bytes(a))) || overlaps_pools(a, x, x) ||
-         overlaps(a, x, a.block_tables, (uint64_t)a.S * a.MAXB * 4) || overlaps(a, x, a.context_lens, (uint64_t)a.S * 4);
-}
-
-// One layer.  Where it writes into its own inputs the rows are kept at the end of the workspace's room for records until all
-// is read: a layer's records and words leave three quarters of it.
-static int launch_layer(pkv::AttnLaunch a, const pkv::AttnLayer& layer, hipStream_t st) {
-  a.layer = layer;
-  if (!writes_own_input(a, layer)) return launch_attn(a, nullptr, st);
-  a.layer.out = reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(a.ws_rec + record_slots(a.S, a.Hkv) * pkv::record_floats(a.G, a.D)) - row_bytes(a));
-  const int rc = launch_attn(a, nullptr, st);
-  if (rc != PKV_OK) return rc;
-  return launch_status(pkv::launch_copy(a.layer.out, layer.out, row_bytes(a), st));
-}
-
 int paged_decode_attn(const void* q, const void* k_pool, const void* v_pool,
                       const int32_t* block_tables, const int32_t* context_lens, float scale,
                       void* out, const pkv_attn_shape* shape, void* workspace,
                       size_t workspace_bytes_given, void* stream) {
   pkv::AttnLaunch a;
   bool empty = false;
-  int rc = prepare_attn(block_tables, context_lens, scale, false, shape, workspace, workspace_bytes_given,
+  int rc = prepare_attn(block_tables, context_lens, scale, 0, nullptr, shape, workspace, workspace_bytes_given,
                         &a, &empty);
   if (rc != PKV_OK || empty) return rc;
   rc = check_layer_pointers(q, k_pool, v_pool, out);
   if (rc != PKV_OK) return rc;
-  return launch_layer(a, layer_of(q, k_pool, v_pool, out), static_cast<hipStream_t>(stream));
+  return launch_layer(a, layer_of(q, k_pool, v_pool, out), static_cast<hipStream_t>(stream), launch_attn_stream);
 }
 
 int paged_decode_attn_fp8kv(const void* q, const void* k_pool, const void* v_pool,
@@ -298,7 +116,7 @@ int paged_decode_attn_fp8kv(const void* q, const void* k_pool, const void* v_poo
     return PKV_ERR_SHAPE;
   pkv::AttnLaunch a;
   bool empty = false;
-  rc = prepare_attn(block_tables, context_lens, scale, true, shape, workspace, workspace_bytes_given, &a,
+  rc = prepare_attn(block_tables, context_lens, scale, 1, nullptr, shape, workspace, workspace_bytes_given, &a,
                     &empty);
   if (rc != PKV_OK || empty) return rc;
   rc = check_layer_pointers(q, k_pool, v_pool, out);
@@ -307,7 +125,7 @@ int paged_decode_attn_fp8kv(const void* q, const void* k_pool, const void* v_poo
   // to the normalised row
   a.scale_log2e = scale * k_scale * 1.4426950408889634f;
   a.out_scale = v_scale;
-  return launch_layer(a, layer_of(q, k_pool, v_pool, out), static_cast<hipStream_t>(stream));
+  return launch_layer(a, layer_of(q, k_pool, v_pool, out), static_cast<hipStream_t>(stream), launch_attn_stream);
 }
 
 int paged_decode_attn_static(const void* q, const void* k_pool, const void* v_pool,
@@ -325,9 +143,9 @@ int paged_decode_attn_static(const void* q, const void* k_pool, const void* v_po
   if (rc != PKV_OK) return rc;
   pkv::AttnLaunch a;
   bool empty = false;
-  rc = prepare_attn(block_tables, context_lens, scale, false, shape, ws, kStaticScratchBytes, &a, &empty);
+  rc = prepare_attn(block_tables, context_lens, scale, 0, nullptr, shape, ws, kStaticScratchBytes, &a, &empty);
   if (rc != PKV_OK || empty) return rc;
-  return launch_layer(a, layer_of(q, k_pool, v_pool, out), static_cast<hipStream_t>(stream));
+  return launch_layer(a, layer_of(q, k_pool, v_pool, out), static_cast<hipStream_t>(stream), launch_attn_stream);
 }
 
 int paged_decode_attn_layers(const void* const* q, const void* const* k_pools,
@@ -338,7 +156,7 @@ int paged_decode_attn_layers(const void* const* q, const void* const* k_pools,
   if (num_layers < 0) return PKV_ERR_SHAPE;
   pkv::AttnLaunch a;
   bool empty = false;
-  int rc = prepare_attn(block_tables, context_lens, scale, false, shape, workspace, workspace_bytes_given,
+  int rc = prepare_attn(block_tables, context_lens, scale, 0, nullptr, shape, workspace, workspace_bytes_given,
                         &a, &empty);
   if (rc != PKV_OK || empty || num_layers == 0) return rc;
   if (!q || !k_pools || !v_pools || !out) return PKV_ERR_NULL;
@@ -370,8 +188,8 @@ int paged_decode_attn_layers(const void* const* q, const void* const* k_pools,
       layers.layer[layers.count++] = y;
       if (writes_own_input(a, y)) break;
     }
-    rc = layers.count > 1 ? launch_attn(a, &layers, static_cast<hipStream_t>(stream))
-                          : launch_layer(a, layers.layer[0], static_cast<hipStream_t>(stream));
+    rc = layers.count > 1 ? launch_attn(a, &layers, static_cast<hipStream_t>(stream), launch_attn_stream)
+                          : launch_layer(a, layers.layer[0], static_cast<hipStream_t>(stream), launch_attn_stream);
     if (rc != PKV_OK) return rc;
   }
   return PKV_OK;

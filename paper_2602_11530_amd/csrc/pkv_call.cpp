@@ -17,7 +17,7 @@
 namespace {
 
 PyObject *s_data_ptr, *s_numel, *s_element_size, *s_cuda_stream;   // names of methods and an attribute
-PyObject *g_shape_type, *g_initialized, *g_device, *g_raw_stream;
+PyObject *g_shape_type, *g_rope_type, *g_initialized, *g_device, *g_raw_stream;
 
 // An int's value, false if it is no int.
 bool take_int(PyObject* o, int64_t* out) {
@@ -64,15 +64,20 @@ struct Real {
     return true;
   }
 };
-struct Shape {
+template <typename C, PyObject** kType>
+struct Struct {   // an object of that ctypes class
   Py_buffer view = {};
   bool take(PyObject* o) {
-    return Py_IS_TYPE(o, (PyTypeObject*)g_shape_type) && PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) == 0 &&
-           view.len == (Py_ssize_t)sizeof(pkv_attn_shape);
+    return Py_IS_TYPE(o, (PyTypeObject*)*kType) && PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) == 0 && view.len == (Py_ssize_t)sizeof(C);
   }
-  ~Shape() {
+  ~Struct() {
     if (view.obj) PyBuffer_Release(&view);
   }
+};
+using Shape = Struct<pkv_attn_shape, &g_shape_type>;
+using Rope = Struct<pkv_rope_shape, &g_rope_type>;
+struct Number32 : Number {   // of those that do not fit ctypes takes the lower bits; they are left to it
+  bool take(PyObject* o) { return Number::take(o) && v == (int32_t)v; }
 };
 struct Stream {   // a handle, an object that has one, or None for the current device's current stream
   void* p = nullptr;
@@ -113,7 +118,9 @@ std::tuple<AnyPointer> c_args(const Address& a) { return {AnyPointer{a.p}}; }
 std::tuple<AnyPointer, size_t> c_args(const Workspace& a) { return {AnyPointer{a.p}, a.bytes}; }
 std::tuple<int64_t> c_args(const Number& a) { return {a.v}; }
 std::tuple<float> c_args(const Real& a) { return {a.v}; }
-std::tuple<const pkv_attn_shape*> c_args(const Shape& a) { return {(const pkv_attn_shape*)a.view.buf}; }
+std::tuple<int32_t> c_args(const Number32& a) { return {(int32_t)a.v}; }
+template <typename C, PyObject** kType>
+std::tuple<const C*> c_args(const Struct<C, kType>& a) { return {(const C*)a.view.buf}; }
 std::tuple<void*> c_args(const Stream& a) { return {a.p}; }
 
 template <typename... A, typename Fn, size_t... I>
@@ -135,8 +142,8 @@ PyObject* call(Fn fn, PyObject* const* args, std::index_sequence<I...>) {
   return PyLong_FromLong(status);
 }
 
-// One entry point: its address, once known, and the kinds of its arguments in order.
-template <typename F, typename... A>
+// One entry point: its address, once known, and the kinds of its arguments in order.  A line each: two may have the same type.
+template <int kLine, typename F, typename... A>
 struct Entry {
   static inline F* fn = nullptr;
   static PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -145,16 +152,25 @@ struct Entry {
   }
 };
 using T = Address;
-using Append = Entry<decltype(kv_append), T, T, T, T, T, T, Shape, Stream>;
-using AppendFp8 = Entry<decltype(kv_append_fp8), T, T, T, T, T, T, Real, Real, Shape, Stream>;
-using Attn = Entry<decltype(paged_decode_attn), T, T, T, T, T, Real, T, Shape, Workspace, Stream>;
-using AttnFp8 = Entry<decltype(paged_decode_attn_fp8kv), T, T, T, T, T, Real, Real, Real, T, Shape, Workspace, Stream>;
-using AttnStatic = Entry<decltype(paged_decode_attn_static), T, T, T, T, T, Real, T, Shape, Stream>;
-using Gather = Entry<decltype(kv_blocks_gather), T, T, T, Number, Number, Number, Stream>;
-using Scatter = Entry<decltype(kv_blocks_scatter), T, T, T, Number, Number, Number, Stream>;
-using Move = Entry<decltype(kv_blocks_move), T, T, T, T, Number, Number, Number, Number, Stream>;
-using Offload = Entry<decltype(kv_blocks_offload), T, T, T, T, Number, Number, Number, Stream>;
-using Reload = Entry<decltype(kv_blocks_reload), T, T, T, T, Number, Number, Number, Stream>;
+using Append = Entry<__LINE__, decltype(kv_append), T, T, T, T, T, T, Shape, Stream>;
+using AppendFp8 = Entry<__LINE__, decltype(kv_append_fp8), T, T, T, T, T, T, Real, Real, Shape, Stream>;
+using Attn = Entry<__LINE__, decltype(paged_decode_attn), T, T, T, T, T, Real, T, Shape, Workspace, Stream>;
+using AttnFp8 = Entry<__LINE__, decltype(paged_decode_attn_fp8kv), T, T, T, T, T, Real, Real, Real, T, Shape, Workspace, Stream>;
+using AttnStatic = Entry<__LINE__, decltype(paged_decode_attn_static), T, T, T, T, T, Real, T, Shape, Stream>;
+using AppendFp4 = Entry<__LINE__, decltype(kv_append_fp4), T, T, T, T, T, T, Shape, Stream>;
+using AttnFp4 = Entry<__LINE__, decltype(paged_decode_attn_fp4kv), T, T, T, T, T, Real, T, Shape, Workspace, Stream>;
+using N = Number32;
+using Span = Entry<__LINE__, decltype(paged_decode_attn_window), T, T, T, T, T, Real, N, N, T, Shape, Workspace, Stream>;
+using SpanFp8 = Entry<__LINE__, decltype(paged_decode_attn_window_fp8kv), T, T, T, T, T, Real, Real, Real, N, N, T, Shape, Workspace, Stream>;
+using SpanFp4 = Entry<__LINE__, decltype(paged_decode_attn_window_fp4kv), T, T, T, T, T, Real, N, N, T, Shape, Workspace, Stream>;
+using RopeBf16 = Entry<__LINE__, decltype(kv_rope_append), T, T, T, T, T, T, T, T, T, T, T, T, Rope, Shape, Stream>;
+using RopeFp8 = Entry<__LINE__, decltype(kv_rope_append_fp8), T, T, T, T, T, T, T, T, T, T, T, T, Real, Real, Rope, Shape, Stream>;
+using RopeFp4 = Entry<__LINE__, decltype(kv_rope_append_fp4), T, T, T, T, T, T, T, T, T, T, T, T, Rope, Shape, Stream>;
+using Gather = Entry<__LINE__, decltype(kv_blocks_gather), T, T, T, Number, Number, Number, Stream>;
+using Scatter = Entry<__LINE__, decltype(kv_blocks_scatter), T, T, T, Number, Number, Number, Stream>;
+using Move = Entry<__LINE__, decltype(kv_blocks_move), T, T, T, T, Number, Number, Number, Number, Stream>;
+using Offload = Entry<__LINE__, decltype(kv_blocks_offload), T, T, T, T, Number, Number, Number, Stream>;
+using Reload = Entry<__LINE__, decltype(kv_blocks_reload), T, T, T, T, Number, Number, Number, Stream>;
 
 template <typename E>
 void set_address(PyObject* addresses, const char* name) {
@@ -163,11 +179,12 @@ void set_address(PyObject* addresses, const char* name) {
   E::fn = o && take_int(o, &x) ? (decltype(E::fn))x : nullptr;
 }
 
-// setup(addresses of the C functions by name, the class of shapes, and three functions of torch or None: is the GPU initialised, the
+// setup(addresses of the C functions by name, the classes of the two kinds of shapes, and three functions of torch or None: is the GPU initialised, the
 // current device, the handle of its current stream)
 PyObject* setup(PyObject*, PyObject* args) {
-  PyObject *addresses, *shape, *initialized, *device, *raw;
-  if (!PyArg_ParseTuple(args, "O!O!OOO", &PyDict_Type, &addresses, &PyType_Type, &shape, &initialized, &device, &raw)) return nullptr;
+  PyObject *addresses, *shape, *rope, *initialized, *device, *raw;
+  if (!PyArg_ParseTuple(args, "O!O!O!OOO", &PyDict_Type, &addresses, &PyType_Type, &shape, &PyType_Type, &rope, &initialized, &device, &raw))
+    return nullptr;
   set_address<Append>(addresses, "kv_append");
   set_address<AppendFp8>(addresses, "kv_append_fp8");
   set_address<Attn>(addresses, "paged_decode_attn");
@@ -178,8 +195,16 @@ PyObject* setup(PyObject*, PyObject* args) {
   set_address<Move>(addresses, "kv_blocks_move");
   set_address<Offload>(addresses, "kv_blocks_offload");
   set_address<Reload>(addresses, "kv_blocks_reload");
+  set_address<AppendFp4>(addresses, "kv_append_fp4");
+  set_address<AttnFp4>(addresses, "paged_decode_attn_fp4kv");
+  set_address<Span>(addresses, "paged_decode_attn_window");
+  set_address<SpanFp8>(addresses, "paged_decode_attn_window_fp8kv");
+  set_address<SpanFp4>(addresses, "paged_decode_attn_window_fp4kv");
+  set_address<RopeBf16>(addresses, "kv_rope_append");
+  set_address<RopeFp8>(addresses, "kv_rope_append_fp8");
+  set_address<RopeFp4>(addresses, "kv_rope_append_fp4");
   const std::pair<PyObject**, PyObject*> keep[] = {
-      {&g_shape_type, shape}, {&g_initialized, initialized}, {&g_device, device}, {&g_raw_stream, raw}};
+      {&g_shape_type, shape}, {&g_rope_type, rope}, {&g_initialized, initialized}, {&g_device, device}, {&g_raw_stream, raw}};
   for (auto& k : keep) {
     Py_INCREF(k.second);
     PyObject* old = *k.first;
@@ -205,6 +230,14 @@ PyMethodDef methods[] = {
     method<Move>("kv_blocks_move"),
     method<Offload>("kv_blocks_offload"),
     method<Reload>("kv_blocks_reload"),
+    method<AppendFp4>("kv_append_fp4"),
+    method<AttnFp4>("paged_decode_attn_fp4kv"),
+    method<Span>("paged_decode_attn_window"),
+    method<SpanFp8>("paged_decode_attn_window_fp8kv"),
+    method<SpanFp4>("paged_decode_attn_window_fp4kv"),
+    method<RopeBf16>("kv_rope_append"),
+    method<RopeFp8>("kv_rope_append_fp8"),
+    method<RopeFp4>("kv_rope_append_fp4"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pkv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

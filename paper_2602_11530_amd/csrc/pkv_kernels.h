@@ -144,6 +144,7 @@ struct AttnLayer {
   uint16_t* out;
 };
 constexpr int kMaxLaunchLayers = 8;
+constexpr int kFp4Pools = 2;
 
 struct AttnLaunch {
   AttnLayer layer;
@@ -155,7 +156,7 @@ struct AttnLaunch {
   int short_blocks;    // see short_segment()
   float scale_log2e;   // softmax scale x log2(e) (x the K pool's scale for an e4m3 pool)
   float out_scale;     // applied to the normalised row: 1, or the V pool's scale
-  int kv_fp8;          // the pools hold one-byte e4m3 values
+  int kv_fp8;          // the pools hold one-byte e4m3 values (1), E2M1 tiles (kFp4Pools)
   int32_t* id_faults;  // optional device counter of refused block ids (nullptr: not reported)
   int S, Hq, Hkv, G, MAXB;
   int D;           // head dimension: 64, 128 or 256
@@ -177,6 +178,41 @@ struct AttnLayers {
 };
 struct OneLayer {};
 struct WholeLayer : OneLayer {};   // a workgroup for each segment
+// Which tokens a request of L sees: its last `window`, and its first `sinks`.  Both are at most the longest context.  Of its 16-token units
+// those that hold such a token are attended over, in order; what lies between the sinks and the window is no part of the stream.
+struct Span {
+  int window, sinks;
+  __host__ __device__ static int units_of(int n) { return (int)(((uint32_t)n + kBlockTokens - 1) / kBlockTokens); }
+  __host__ __device__ int sink_units() const { return units_of(sinks); }
+  // units left out behind the sinks'
+  __host__ __device__ int left_out(int L) const {
+    const int first = L > window ? L - window : 0;   // of the window; behind the last token where there is none
+    const int n = (window > 0 ? first / kBlockTokens : units_of(first)) - sink_units();
+    return n > 0 ? n : 0;
+  }
+  __host__ __device__ int units(int L) const { return units_of(L) - left_out(L); }
+  // of a request of at most `tokens`
+  int64_t most_units(int tokens) const {
+    const int64_t all = units_of(tokens), some = (int64_t)sink_units() + (window > 0 ? units_of(window) + 1 : 0);
+    return all < some ? all : some;
+  }
+  // the request's unit that is the b-th of those
+  __host__ __device__ int unit(int b, int L) const { return b < sink_units() ? b : b + left_out(L); }
+  // of its tokens the seen ones, a bit each
+  __host__ __device__ uint32_t seen(int unit, int L) const {
+    const int at = kBlockTokens * unit, first = L > window ? L - window : 0;
+    return below(L - at) & (below(sinks - at) | ~below(first - at));
+  }
+  __host__ __device__ static uint32_t below(int n) { return (1u << (n < 0 ? 0 : n > kBlockTokens ? kBlockTokens : n)) - 1; }
+};
+// A layer of requests that see part of their context.
+struct SpanLayer : OneLayer {
+  Span span;
+};
+// Pools of E2M1 tiles (fp4.h).
+struct Fp4Pools {};
+struct Fp4Layer : OneLayer, Fp4Pools {};
+struct Fp4SpanLayer : SpanLayer, Fp4Pools {};
 // One after the other in each workgroup.
 struct ChainedLayers : AttnLayers {};
 __device__ __forceinline__ int layer_index(const OneLayer&) { return 0; }
@@ -256,6 +292,9 @@ inline bool short_at_128(const AttnLaunch& a) {
   const int64_t most = (int64_t)a.S * a.Hkv * ((a.max_ctx + kBlockTokens - 1) / kBlockTokens);
   return a.D == 128 && !a.kv_fp8 && most <= 16 * (int64_t)a.waves;
 }
+// The stream pass over E2M1 tiles, or for requests that see part of their context, or both.  `span`: nullptr for all of it.
+hipError_t launch_attn_span(const AttnLaunch& a, const Span* span, hipStream_t stream);
+hipError_t launch_attn_fp4(const AttnLaunch& a, const Span* span, size_t lds, hipStream_t stream);   // with LDS laid out
 // The stream pass's kernels for one layer of those, and for layers one after the other.
 void launch_large_256(const AttnLaunch& a, size_t lds, hipStream_t stream);
 void launch_short_128(const AttnLaunch& a, size_t lds, hipStream_t stream);
@@ -308,6 +347,24 @@ hipError_t launch_kv_append_fp8(const uint16_t* k_new, const uint16_t* v_new, vo
                                 const int32_t* context_lens, float k_scale, float v_scale, int S,
                                 int Hkv, int D, int MAXB, int B, int max_ctx, int NB,
                                 int32_t* id_faults, hipStream_t stream);
+
+// New tokens: queries and keys normalised and rotated, keys and values into their slots (kv_rope.hip).
+struct RopeLaunch {
+  const uint16_t *q, *k, *v;             // a token's heads in a row, tokens that many elements apart:
+  int64_t q_stride, k_stride, v_stride;
+  const uint16_t *q_norm, *k_norm;       // weights [D]; nullptr: as they are
+  const float* cos_sin;                  // [positions][R]
+  uint16_t* q_out;
+  void *k_pool, *v_pool;
+  const int32_t *block_tables, *context_lens;
+  const int32_t* token_starts;           // [S + 1]; nullptr: token s is request s's last one
+  int32_t* id_faults;
+  float eps, k_scale, v_scale;
+  int kv_fp8;                            // as in AttnLaunch
+  int T, S, Hq, Hkv, D, R, interleaved;
+  int MAXB, log_block, max_ctx, NB;
+};
+hipError_t launch_kv_rope(const RopeLaunch& a, hipStream_t stream);
 
 // Measurement aid: the stream pass's loads at D = 128 in bf16 with no arithmetic (see stream_probe.hip).
 hipError_t launch_stream_read_probe(const void* k_buf, const void* v_buf, uint32_t num_slabs,

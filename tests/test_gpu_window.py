@@ -1,0 +1,152 @@
+"""Attention over a window and sinks against a plain implementation in 64 bits, over all three kinds of pools: masks that end inside blocks, rows
+that see nothing, NaN in what is not seen, freed blocks, odd head groups, many requests."""
+import numpy as np
+import pytest
+import torch
+
+import plain
+from formats_util import KINDS, attend, make_batch, pools_of, poison
+from gpu_util import to_bits, to_dev
+from paper_2602_11530_amd import binding as pkv
+from paper_2602_11530_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+LENS = [0, 1, 15, 16, 17, 33, 100, 5, 257, 600, 64, 48]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim,block", [(64, 32), (128, 16), (256, 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (16, 0), (50, 4), (33, 20), (7, 16), (40, 100), (10000, 3), (0, 5), (0, 0), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_masks(device, kind, dim, block, window, sinks):
+    b = make_batch(LENS, 8, 2, dim, block, seed=dim + window % 1000 + sinks % 1000)
+    pools = pools_of(b, kind)
+    got = attend(b, pools, window=window, sinks=sinks)
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, window, sinks)
+    plain.within(got, want, off)
+    nothing = [s for s, n in enumerate(LENS) if n == 0 or window == sinks == 0]
+    assert (got[nothing] == 0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (5, 1), (28, 4), (12, 12), (32, 4)])
+def test_head_groups(device, kind, dim, hq, hkv):
+    b = make_batch([900, 31, 2, 400, 1500], hq, hkv, dim, 16, seed=hq)
+    pools = pools_of(b, kind)
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, 300, 6)
+    plain.within(attend(b, pools, window=300, sinks=6), want, off)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_what_is_not_seen_does_not_matter(device, kind, dim):
+    """NaN in tokens that are not seen, in unused slots and blocks, and no block at all where none is seen."""
+    window, sinks = 37, 9
+    b = make_batch(LENS, 4, 2, dim, 16, seed=9, spare=5)
+    pools = pools_of(b, kind)
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, window, sinks)
+    seen = np.zeros((b.num_blocks, 16), bool)
+    for s, n in enumerate(b.lens):
+        for t in range(n):
+            seen[b.tables[s, t // 16], t % 16] |= t >= n - window or t < sinks
+    poison(pools, kind, ~seen)
+    freed = b.tables.copy()
+    for s, n in enumerate(b.lens):
+        for j in range(b.tables.shape[1]):
+            t = np.arange(16 * j, 16 * j + 16)
+            if not ((t < n) & ((t >= n - window) | (t < sinks))).any():
+                freed[s, j] = (-1, b.num_blocks, 2 ** 31 - 1)[j % 3]
+    b.tables = freed
+    plain.within(attend(b, pools, window=window, sinks=sinks), want, off)
+
+
+def test_nan_that_is_seen(device):
+    b = make_batch([100, 100, 100], 4, 2, 128, 16, seed=3)
+    pools = pools_of(b, "bf16")
+    k, v = pools.k_bits.copy(), pools.v_bits.copy()
+    k[b.tables[0, 0], 0, 2] = wl.BF16_NAN              # a sink of request 0, head 0
+    v[b.tables[1, 6], 1, 3, 7] = wl.BF16_NAN           # token 99 of request 1, head 1
+    v[b.tables[2, 3], 1, 0] = wl.BF16_NAN              # token 48 of request 2: not seen
+    pools.k_dev, pools.v_dev = to_dev(k), to_dev(v)
+    out = wl.bf16_bits_to_f64(attend(b, pools, window=20, sinks=4)).reshape(3, 4, 128)
+    nan = np.isnan(out)
+    want = np.zeros_like(nan)
+    want[0, :2] = True
+    want[1, 2:, 7] = True
+    assert np.array_equal(nan, want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("seqs,hkv,longest", [(70, 2, 300), (300, 1, 120), (3, 2, 9000), (2048, 1, 20)])
+def test_many_requests_and_long_ones(device, kind, dim, seqs, hkv, longest):
+    rng = np.random.default_rng(seqs)
+    b = make_batch(rng.integers(0, longest + 1, seqs), 2 * hkv, hkv, dim, 16, seed=seqs)
+    pools = pools_of(b, kind)
+    window = longest // 3 + 1
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, window, 18)
+    plain.within(attend(b, pools, window=window, sinks=18), want, off)
+    plain.within(attend(b, pools, window=window, sinks=18, max_context_len=int(b.lens.max())), want, off)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_length_bound(device, kind):
+    """A request longer than the bound is attended as if it had that length."""
+    b = make_batch([300, 90, 200], 4, 2, 128, 16, seed=6)
+    pools = pools_of(b, kind)
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, np.minimum(b.lens, 128), b.scale, 50, 4)
+    plain.within(attend(b, pools, window=50, sinks=4, max_context_len=128), want, off)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_partitions(device, kind):
+    b = make_batch([1000, 90, 3000], 8, 2, 128, 16, seed=8)
+    pools = pools_of(b, kind)
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, 700, 40)
+    plain.within(attend(b, pools, window=700, sinks=40, partition_size=64), want, off)
+
+
+@pytest.mark.expects_id_faults
+@pytest.mark.parametrize("kind", KINDS)
+def test_ids_outside_the_pool(device, id_faults, kind):
+    b = make_batch([200, 90, 50], 4, 2, 128, 16, seed=11)
+    pools = pools_of(b, kind)
+    b.tables[0, 0], b.tables[0, 11] = -7, b.num_blocks       # a sink block, and one of the window
+    b.tables[0, 5] = b.num_blocks + 9                        # not seen
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, 32, 4)
+    plain.within(attend(b, pools, window=32, sinks=4), want, off)
+    assert int(id_faults.item()) == 2 * 2                    # two units, two KV heads
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_output_over_its_inputs(device, kind):
+    b = make_batch([200, 90, 50, 700], 4, 2, 128, 16, seed=12)
+    pools = pools_of(b, kind)
+    want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, 64, 4)
+    q = to_dev(b.q_bits)
+    plain.within(attend(b, pools, window=64, sinks=4, q=q, out=q), want, off)
+    # the rows over the beginning of V's pool, which is read before they are written
+    out = pools.v_dev.view(-1).view(torch.int16)[:b.q.size].view(b.q.shape)
+    plain.within(attend(b, pools, window=64, sinks=4, out=out), want, off)
+
+
+def test_two_streams_with_a_workspace_each(device):
+    b = make_batch([3000, 90, 1500, 2000], 8, 2, 128, 16, seed=13)
+    pools = pools_of(b, "bf16")
+    once = attend(b, pools, window=900, sinks=4)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[attend(b, pools, window=900, sinks=4, stream=s, wait=False) for _ in range(8)] for s in streams]
+    torch.cuda.synchronize()
+    for o in outs[0] + outs[1]:
+        assert np.array_equal(to_bits(o), once)
+
+
+def test_binding_refuses(device):
+    b = make_batch([20], 4, 2, 128, 16, seed=14)
+    pools = pools_of(b, "bf16")
+    for bad in (dict(window=-1, sinks=0), dict(window=1, sinks=-1)):
+        with pytest.raises(pkv.PkvError) as e:
+            attend(b, pools, **bad)
+        assert e.value.status == pkv.PKV_ERR_SHAPE
