@@ -119,9 +119,11 @@ template <> struct Dim<256, true> {
   typedef uint32_t VReg __attribute__((ext_vector_type(2)));
 };
 // E2M1 codes with a scale for each 32 dims (tiles, fp4.h), widened to bf16 in registers (exactly, scale and all).  K: a lane has 32 dims of token
-// n, 16 at D = 64; V: the lane's dims of tokens 4*c .. 4*c + 3, in one load (one for each half at D = 256).
+// n, 16 at D = 64; V: the lane's dims of tokens 4*c .. 4*c + 3, in one load (one for each half at D = 256).  Two tiles at a time: the loads
+// of both are one block's here.
 template <int kD> struct Fp4Dim {
-  static constexpr int kKSteps = kD / 32, kKLoads = kD == 256 ? 2 : 1, kVLoads = kKLoads, kTiles = kD / 16, kElemBytes = 1;
+  static constexpr int kPerTile = kD == 256 ? 2 : 1;   // loads
+  static constexpr int kKSteps = kD / 32, kKLoads = 2 * kPerTile, kVLoads = kKLoads, kTiles = kD / 16, kElemBytes = 1;
   typedef uint32_t Codes __attribute__((ext_vector_type(kD == 64 ? 2 : 4)));
   struct Load {
     Codes codes;
@@ -157,7 +159,7 @@ __device__ __forceinline__ u32x2 widen_e4m3x4(uint32_t w) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true))};
 }
 
-// The bf16 pairs of a dword of eight codes, times the scale (its exponent counts; 255 gives NaN).
+// The bf16 pairs of a dword of eight codes, times the scale: bits 23 to 30 of it alone count, 255 there gives NaN.
 __device__ __forceinline__ u32x4 widen_e2m1x8(uint32_t w, float scale) {
   return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
@@ -216,6 +218,30 @@ constexpr int kMetaSegFirst = 1 << 9;   // first block of its segment in this sh
 constexpr int kMetaSegEnd = 1 << 10;    // last block of its segment
 constexpr int kMetaOpenLeft = 1 << 11;  // its segment begins before this share
 
+// Pairs of tiles: a run's tiles two by two, the last one by itself if their number is odd or it is the last of its window.
+template <typename Block>
+struct PairOfTiles {
+  Block first, second;
+  int seg, j;   // of the first
+};
+struct PairWalk {
+  int j;            // stream index of the next pair
+  bool described;   // is window B?
+};
+template <typename Block>
+__device__ __forceinline__ PairOfTiles<Block> next_pair(Window& a, const Window& b, int& jbase, PairWalk& walk) {
+  if (walk.j == jbase + kWindow) {   // the loads leave window A: B becomes A
+    a = b;
+    jbase += kWindow;
+    walk.described = false;
+  }
+  auto block_at = [&](int j) { return Block{__builtin_amdgcn_readlane(a.slab, j - jbase), __builtin_amdgcn_readlane(a.meta, j - jbase)}; };
+  PairOfTiles<Block> p = {block_at(walk.j), {0, 0}, __builtin_amdgcn_readlane(a.seg, walk.j - jbase), walk.j};
+  ++walk.j;
+  if (!(p.first.meta & kMetaLast) && walk.j < jbase + kWindow) p.second = block_at(walk.j++);
+  return p;
+}
+
 // How a wavefront's share ends.
 constexpr int kEndsLeft = 1;      // the left record is in use: the first segment begins before the share
 constexpr int kEndsThrough = 2;   // and goes on after it
@@ -265,7 +291,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   constexpr bool kWhole = std::is_base_of_v<WholeLayer, Layers>;
   constexpr int kNextK = kD == 128 && (!kLarge || std::is_same_v<Layers, AttnLayers>) ? kKLoads : kAhead;
   // the next block's loads go out before this one's have arrived
-  constexpr bool kTwoBlocks = kFp4 ? kD <= 128 : kD == 64 && kFp8;
+  constexpr bool kTwoBlocks = !kFp4 && kD == 64 && kFp8;
   constexpr int kGroupWaves = group_waves(kD), kThreads = kGroupWaves * 64;
   extern __shared__ __align__(16) int smem[];
   int* cumB = smem;                  // [S+1] blocks before request s
@@ -564,14 +590,16 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
                                              kFp4 ? ((at.meta & 0xff) ? fp4_tile_bytes(kD) : 0) : (at.meta & 0xff) * (kD * kElemBytes),
                                              kRawBuffer);
   };
+  // (a pair of tiles: the loads of one of them, `from` being 0 or kPerTile)
   auto issue_k = [&](KReg (&k)[kKLoads], Block at, int from, int to) {
     const __amdgpu_buffer_rsrc_t b = rows_of(layer.k_pool, at);
     if constexpr (kFp4) {
       typedef typename DD::Codes Codes;
 #pragma unroll
-      for (int jj = from; jj < to; ++jj) {
-        k[jj].codes = load_nt<Codes>(b, kD == 64 ? 256 * (c >> 1) + 16 * n + 8 * (c & 1) : 16 * (64 * jj + lane));
-        k[jj].scales = load_nt<uint8_t>(b, 8 * kD + (kD == 64 ? 16 * (c >> 1) + n : 64 * jj + lane));
+      for (int z = from; z < to; ++z) {
+        const int jj = z - from;
+        k[z].codes = load_nt<Codes>(b, kD == 64 ? 256 * (c >> 1) + 16 * n + 8 * (c & 1) : 16 * (64 * jj + lane));
+        k[z].scales = load_nt<uint8_t>(b, 8 * kD + (kD == 64 ? 16 * (c >> 1) + n : 64 * jj + lane));
       }
     } else if (turns) {
 #pragma unroll
@@ -581,15 +609,15 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       for (int jj = from; jj < to; ++jj) k[jj] = load_nt<u32x4>(b, 16 * (koff + 4 * jj));
     }
   };
-  auto issue_v = [&](VReg (&v)[kVLoads], Block at) {
+  auto issue_v = [&](VReg (&v)[kVLoads], Block at, int from = 0) {
     const __amdgpu_buffer_rsrc_t b = rows_of(layer.v_pool, at);
     constexpr int kBytes = sizeof(VReg);
     if constexpr (kFp4) {
       typedef typename DD::Codes Codes;
 #pragma unroll
-      for (int h = 0; h < kVLoads; ++h) {
-        v[h].codes = load_nt<Codes>(b, (int)sizeof(Codes) * (kD == 256 ? 32 * c + 16 * h + n : lane));
-        v[h].scales = load_nt<uint32_t>(b, 8 * kD + 16 * (kD == 64 ? n >> 3 : 4 * h + (n >> 2)) + 4 * c);
+      for (int h = 0; h < DD::kPerTile; ++h) {
+        v[from + h].codes = load_nt<Codes>(b, (int)sizeof(Codes) * (kD == 256 ? 32 * c + 16 * h + n : lane));
+        v[from + h].scales = load_nt<uint32_t>(b, 8 * kD + 16 * (kD == 64 ? n >> 3 : 4 * h + (n >> 2)) + 4 * c);
       }
     } else if constexpr (kD == 256) {
 #pragma unroll
@@ -600,6 +628,14 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = load_nt<VReg>(b, kBytes * (voff + 64 * e));
+    }
+  };
+  auto issue_pair = [&](KReg (&k)[kKLoads], VReg (&v)[kVLoads], Block first, Block second) {
+    if constexpr (kFp4) {
+      issue_k(k, first, 0, DD::kPerTile);
+      issue_k(k, second, DD::kPerTile, kKLoads);
+      issue_v(v, first);
+      issue_v(v, second, DD::kPerTile);
     }
   };
   // K of a block that has arrived, into LDS and back as the A operand: load L of lane (n, c) is piece 4L + c of token tau(n).
@@ -635,125 +671,221 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     nstaged = 0;
   };
 
-  auto consume = [&](KReg (&kraw)[kKLoads], VReg (&vraw)[kVLoads], int meta) __attribute__((always_inline)) {
-    // The MFMA operands.  bf16 pools: the registers as they are.  e4m3 pools: piece 4L + c of
-    // K's row holds dims 16*(4L + c) .. +15 of token tau(n), which feed steps 2L and 2L + 1 (the
-    // contraction order is free as long as q follows it, see below); a V load holds the same
-    // token and dims as in a bf16 pool, one byte each.
-    u32x4 k[kKSteps];
-    constexpr int kVRows = kD == 256 ? 8 : 4;
-    VOp v[kVRows];
+  // Two tiles of a segment, 32 tokens: `seen` has a bit for each that counts.  Scores of a tile's tokens 4*c .. 4*c + 3 are in lane
+  // (n, c), so P is there as one operand of 32 tokens, tile by tile, and V's operands follow it.
+  // `next` has the loads that take the registers of K and of V over as soon as these are widened.
+  auto attend_pair = [&](KReg (&kraw)[kKLoads], VReg (&vraw)[kVLoads], uint32_t seen, auto next) __attribute__((always_inline)) {
+    if constexpr (kFp4) {
+      constexpr int kPer = kD == 256 ? 2 : 1, kSteps = kKSteps / kPer;   // loads of a tile, steps that one feeds
+      f32x4 sc[2];
 #pragma unroll
-    for (int jj = 0; jj < kKLoads; ++jj) {
-      const auto x = kraw[jj];
-      if constexpr (kFp4) {
-        constexpr int kPer = kKSteps / kKLoads;
+      for (int u = 0; u < 2; ++u) {
+        sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kPer; ++w) k[kPer * jj + w] = widen_e2m1x8(x.codes[w], scale_of(x.scales));
-      } else if constexpr (kFp8) {
-        const u32x2 y[4] = {widen_e4m3x4(x.x), widen_e4m3x4(x.y), widen_e4m3x4(x.z), widen_e4m3x4(x.w)};
-        k[2 * jj] = u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
-        k[2 * jj + 1] = u32x4{y[2].x, y[2].y, y[3].x, y[3].y};
-      } else {
-        k[jj] = x;
-      }
-    }
+        for (int jj = 0; jj < kPer; ++jj) {
+          const float scale = scale_of(kraw[kPer * u + jj].scales);
 #pragma unroll
-    for (int e = 0; e < kVRows; ++e) {
-      if constexpr (kFp4) {
-        // token 4*c + t, in half h at D = 256
-        const int t = kD == 256 ? e >> 1 : e, h = kD == 256 ? e & 1 : 0;
-        const float scale = scale_of((vraw[h].scales >> (8 * t)) & 0xff);
-        if constexpr (kD == 64) {
-          const uint32_t w = vraw[0].codes[t >> 1] >> (16 * (t & 1));
-          v[e] = VOp{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
-                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1))};
-        } else {
-          v[e] = widen_e2m1x8(vraw[h].codes[t], scale);
+          for (int w = 0; w < kSteps; ++w)
+            sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, widen_e2m1x8(kraw[kPer * u + jj].codes[w], scale)),
+                                                            __builtin_bit_cast(bf16x8, qop[kSteps * jj + w]), sc[u], 0, 0, 0);
         }
-      } else if constexpr (!kFp8) {
-        v[e] = vraw[e];
-      } else if constexpr (kD == 64) {
-        v[e] = widen_e4m3x4(vraw[e]);
-      } else {
-        const u32x2 a2 = widen_e4m3x4(vraw[e].x), b2 = widen_e4m3x4(vraw[e].y);
-        v[e] = VOp{a2.x, a2.y, b2.x, b2.y};
       }
-    }
-    const int ntok = meta & 0xff;
-    const uint32_t seen = (uint32_t)meta >> 16;   // with a span
-    // element e of a lane's scores and weights is this token
-    auto token = [&](int e) { return kFp4 ? 4 * c + e : 4 * e + c; };
-
-    f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+      next.k(kraw);
+      const bool edge = seen != 0xffffffffu;
+      const uint32_t mine = seen >> (4 * c);
+      auto valid = [&](int i) { return (mine >> (16 * (i >> 2) + (i & 3))) & 1; };   // token 4*c + i % 4 of tile i / 4
+      uint32_t scales[2][kPer];
 #pragma unroll
-    for (int jj = 0; jj < kKSteps; ++jj)
-      sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[jj]),
-                                                   __builtin_bit_cast(bf16x8, qop[jj]), sc, 0, 0, 0);
-    float x[4] = {sc.x * a.scale_log2e, sc.y * a.scale_log2e, sc.z * a.scale_log2e,
-                  sc.w * a.scale_log2e};
-    const bool edge = kSpan ? seen != 0xffff : ntok < kBlockTokens;
-    bool valid[4] = {true, true, true, true};
-    if (edge) {
-      // Last block of a request, or an unmapped one: the rows behind it are zeros, and their
-      // scores and weights are replaced by select.
+      for (int z = 0; z < 2 * kPer; ++z) scales[z / kPer][z % kPer] = vraw[z].scales;
+      if (edge) {
+        // A weight of zero does not silence a NaN in V, which only a scale can be: scales of what does not count are small.
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        valid[e] = kSpan ? (seen >> token(e)) & 1 : token(e) < ntok;
-        x[e] = valid[e] ? x[e] : kNegInf;
+        for (int u = 0; u < 2; ++u) {
+          uint32_t keep = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) keep |= valid(4 * u + e) ? 0xffu << (8 * e) : 0u;
+#pragma unroll
+          for (int h = 0; h < kPer; ++h) scales[u][h] &= keep;
+        }
       }
-      if constexpr (kSpan || kFp4) {
-        // Rows that are there but not seen, a tile's unused ones: a weight of zero does not silence a NaN in V.
-        constexpr int st = kD == 256 ? 2 : 1;
+      VOp v[2][4 * kPer];   // [tile][token, half]
 #pragma unroll
-        for (int e = 0; e < kVRows; ++e) v[e] = valid[e / st] ? v[e] : VOp{};
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int e = 0; e < 4 * kPer; ++e) {
+          const int t = kPer == 2 ? e >> 1 : e, h = kPer == 2 ? e & 1 : 0;
+          const auto& x = vraw[kPer * u + h];
+          const float scale = __uint_as_float(t == 3 ? scales[u][h] >> 1 : scales[u][h] << (23 - 8 * t));
+          if constexpr (kD == 64) {
+            const uint32_t w = x.codes[t >> 1] >> (16 * (t & 1));
+            v[u][e] = VOp{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1))};
+          } else {
+            v[u][e] = widen_e2m1x8(x.codes[t], scale);
+          }
+        }
       }
-    }
-    const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-    if (__any(mx > m + kLazyLog2)) {
-      float mg = fmaxf(mx, __shfl_xor(mx, 16));
-      mg = fmaxf(mg, __shfl_xor(mg, 32));
-      const float mnew = fmaxf(m, mg);   // finite: some lane of the head saw a valid token
-      const float alpha = __builtin_amdgcn_exp2f(m - mnew);
-      l *= alpha;
-      float ar[4];
+      next.v(vraw);
+      float x[8];   // element 4*u + e: token 4*c + e of tile u
 #pragma unroll
-      for (int r = 0; r < 4; ++r) ar[r] = __shfl(alpha, 4 * c + r);
+      for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3] * a.scale_log2e;
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = valid(i) ? x[i] : kNegInf;
+      }
+      const float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(mx > m + kLazyLog2)) {
+        float mg = fmaxf(mx, __shfl_xor(mx, 16));
+        mg = fmaxf(mg, __shfl_xor(mg, 32));
+        const float mnew = fmaxf(m, mg);   // finite: some lane of the head saw a valid token
+        const float alpha = __builtin_amdgcn_exp2f(m - mnew);
+        l *= alpha;
+        float ar[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ar[r] = __shfl(alpha, 4 * c + r);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          o[i].x *= ar[0]; o[i].y *= ar[1]; o[i].z *= ar[2]; o[i].w *= ar[3];
+        }
+        m = mnew;
+      }
+      float pw[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) pw[i] = __builtin_amdgcn_exp2f(x[i] - m);
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pw[i] = valid(i) ? pw[i] : 0.f;   // m may still be -inf here
+      }
+      l += ((pw[0] + pw[1]) + (pw[2] + pw[3])) + ((pw[4] + pw[5]) + (pw[6] + pw[7]));
+      u32x4 hi, lo;   // P = hi + lo in bf16
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hi[i] = pack_bf16(pw[2 * i], pw[2 * i + 1]);
+        lo[i] = pack_bf16(pw[2 * i] - __uint_as_float(hi[i] << 16), pw[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
+      }
+      const bf16x8 pa = __builtin_bit_cast(bf16x8, hi), pb = __builtin_bit_cast(bf16x8, lo);
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        o[i].x *= ar[0]; o[i].y *= ar[1]; o[i].z *= ar[2]; o[i].w *= ar[3];
+        const int wsel = (i & 7) >> 1, h = kD == 256 ? i >> 3 : 0;
+        const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
+        u32x4 vb;
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {   // tokens 2*(z % 2), + 1 of tile z / 2
+          const int e = kPer * 2 * (z & 1) + h;
+          vb[z] = __builtin_amdgcn_perm(v[z >> 1][e + kPer][wsel], v[z >> 1][e][wsel], sel);
+        }
+        const bf16x8 vop = __builtin_bit_cast(bf16x8, vb);
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, vop, o[i], 0, 0, 0);
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pb, vop, o[i], 0, 0, 0);
       }
-      m = mnew;
     }
-    float pw[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) pw[e] = __builtin_amdgcn_exp2f(x[e] - m);
-    if (edge) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) pw[e] = valid[e] ? pw[e] : 0.f;   // m may still be -inf here
-    }
-    l += (pw[0] + pw[1]) + (pw[2] + pw[3]);
+  };
 
-    // P = hi + lo in bf16.
-    uint32_t hb[4];
-    float lo[4];
+  auto consume = [&](KReg (&kraw)[kKLoads], VReg (&vraw)[kVLoads], int meta, auto... pair) __attribute__((always_inline)) {
+    if constexpr (kFp4) {
+      attend_pair(kraw, vraw, pair...);
+    } else {
+      // The MFMA operands.  bf16 pools: the registers as they are.  e4m3 pools: piece 4L + c of
+      // K's row holds dims 16*(4L + c) .. +15 of token tau(n), which feed steps 2L and 2L + 1 (the
+      // contraction order is free as long as q follows it, see below); a V load holds the same
+      // token and dims as in a bf16 pool, one byte each.
+      u32x4 k[kKSteps];
+      VOp v[kVLoads];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) lo[e] = pw[e] - bf16_round(pw[e], hb[e]);
-    const u32x2 phi = {hb[0] | (hb[1] << 16), hb[2] | (hb[3] << 16)};
-    const u32x2 plo = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3])};
-    const s16x4 pa = __builtin_bit_cast(s16x4, phi);
-    const s16x4 pb = __builtin_bit_cast(s16x4, plo);
+      for (int jj = 0; jj < kKLoads; ++jj) {
+        const u32x4 x = kraw[jj];
+        if constexpr (kFp8) {
+          const u32x2 y[4] = {widen_e4m3x4(x.x), widen_e4m3x4(x.y), widen_e4m3x4(x.z), widen_e4m3x4(x.w)};
+          k[2 * jj] = u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
+          k[2 * jj + 1] = u32x4{y[2].x, y[2].y, y[3].x, y[3].y};
+        } else {
+          k[jj] = x;
+        }
+      }
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-      // tile i needs, for tokens 4*e + c (e = 0..3), the bf16 of its dim: half (i & 1) of
-      // word ((i % 8) >> 1) of the load that holds token e (and, for D = 256, half i / 8)
-      const int wsel = (i & 7) >> 1, h = kD == 256 ? i >> 3 : 0, st = kD == 256 ? 2 : 1;
-      const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
-      const u32x2 vb = {__builtin_amdgcn_perm(v[st + h][wsel], v[h][wsel], sel),
-                        __builtin_amdgcn_perm(v[3 * st + h][wsel], v[2 * st + h][wsel], sel)};
-      const s16x4 vop = __builtin_bit_cast(s16x4, vb);
-      o[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(pa, vop, o[i], 0, 0, 0);
-      o[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(pb, vop, o[i], 0, 0, 0);
+      for (int e = 0; e < kVLoads; ++e) {
+        if constexpr (!kFp8) {
+          v[e] = vraw[e];
+        } else if constexpr (kD == 64) {
+          v[e] = widen_e4m3x4(vraw[e]);
+        } else {
+          const u32x2 a2 = widen_e4m3x4(vraw[e].x), b2 = widen_e4m3x4(vraw[e].y);
+          v[e] = VOp{a2.x, a2.y, b2.x, b2.y};
+        }
+      }
+      const int ntok = meta & 0xff;
+      const uint32_t seen = (uint32_t)meta >> 16;   // with a span
+
+      f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int jj = 0; jj < kKSteps; ++jj)
+        sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[jj]),
+                                                     __builtin_bit_cast(bf16x8, qop[jj]), sc, 0, 0, 0);
+      float x[4] = {sc.x * a.scale_log2e, sc.y * a.scale_log2e, sc.z * a.scale_log2e,
+                    sc.w * a.scale_log2e};
+      const bool edge = kSpan ? seen != 0xffff : ntok < kBlockTokens;
+      bool valid[4] = {true, true, true, true};
+      if (edge) {
+        // Last block of a request, or an unmapped one: the rows behind it are zeros, and their
+        // scores and weights are replaced by select.  Element e of this lane is token 4*e + c.
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          valid[e] = kSpan ? (seen >> (4 * e + c)) & 1 : 4 * e + c < ntok;
+          x[e] = valid[e] ? x[e] : kNegInf;
+        }
+        if constexpr (kSpan) {
+          // Rows that are there but not seen: a weight of zero does not silence a NaN in V.
+          constexpr int st = kD == 256 ? 2 : 1;
+#pragma unroll
+          for (int e = 0; e < kVLoads; ++e) v[e] = valid[e / st] ? v[e] : VOp{};
+        }
+      }
+      const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      if (__any(mx > m + kLazyLog2)) {
+        float mg = fmaxf(mx, __shfl_xor(mx, 16));
+        mg = fmaxf(mg, __shfl_xor(mg, 32));
+        const float mnew = fmaxf(m, mg);   // finite: some lane of the head saw a valid token
+        const float alpha = __builtin_amdgcn_exp2f(m - mnew);
+        l *= alpha;
+        float ar[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) ar[r] = __shfl(alpha, 4 * c + r);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+          o[i].x *= ar[0]; o[i].y *= ar[1]; o[i].z *= ar[2]; o[i].w *= ar[3];
+        }
+        m = mnew;
+      }
+      float pw[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pw[e] = __builtin_amdgcn_exp2f(x[e] - m);
+      if (edge) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pw[e] = valid[e] ? pw[e] : 0.f;   // m may still be -inf here
+      }
+      l += (pw[0] + pw[1]) + (pw[2] + pw[3]);
+
+      // P = hi + lo in bf16.
+      uint32_t hb[4];
+      float lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lo[e] = pw[e] - bf16_round(pw[e], hb[e]);
+      const u32x2 phi = {hb[0] | (hb[1] << 16), hb[2] | (hb[3] << 16)};
+      const u32x2 plo = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3])};
+      const s16x4 pa = __builtin_bit_cast(s16x4, phi);
+      const s16x4 pb = __builtin_bit_cast(s16x4, plo);
+#pragma unroll
+      for (int i = 0; i < kTiles; ++i) {
+        // tile i needs, for tokens 4*e + c (e = 0..3), the bf16 of its dim: half (i & 1) of
+        // word ((i % 8) >> 1) of the load that holds token e (and, for D = 256, half i / 8)
+        const int wsel = (i & 7) >> 1, h = kD == 256 ? i >> 3 : 0, st = kD == 256 ? 2 : 1;
+        const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
+        const u32x2 vb = {__builtin_amdgcn_perm(v[st + h][wsel], v[h][wsel], sel),
+                          __builtin_amdgcn_perm(v[3 * st + h][wsel], v[2 * st + h][wsel], sel)};
+        const s16x4 vop = __builtin_bit_cast(s16x4, vb);
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(pa, vop, o[i], 0, 0, 0);
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(pb, vop, o[i], 0, 0, 0);
+      }
     }
 
     if (meta & kMetaLast) {
@@ -863,10 +995,21 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
 
   KReg kbuf[2][kKLoads];   // two blocks in turn, so that no buffer is ever copied
   VReg vbuf[2][kVLoads];
-  Block at = block_at(0);
-  issue_k(kbuf[0], at, 0, kKLoads);
-  if (!kLate) issue_v(vbuf[0], at);
-  if (!kWhole) load_q(__builtin_amdgcn_readlane(dA.seg, 0));
+  [[maybe_unused]] std::conditional_t<kFp4, PairOfTiles<Block>, int> now, then;
+  [[maybe_unused]] PairWalk walk = {0, false};
+  Block at;
+  if constexpr (kFp4) {
+    now = next_pair<Block>(dA, dB, jbase, walk);
+    issue_pair(kbuf[0], vbuf[0], now.first, now.second);
+    if (!kWhole) load_q(now.seg);
+    then = next_pair<Block>(dA, dB, jbase, walk);
+    issue_pair(kbuf[1], vbuf[1], then.first, then.second);
+  } else {
+    at = block_at(0);
+    issue_k(kbuf[0], at, 0, kKLoads);
+    if (!kLate) issue_v(vbuf[0], at);
+    if (!kWhole) load_q(__builtin_amdgcn_readlane(dA.seg, 0));
+  }
   if (wave == 0 && kLeavesWords) {
     // Word for the reduce pass, while the first loads are on their way: the segment of the workgroup's
     // last block, does it go on elsewhere?
@@ -881,7 +1024,42 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     if (lane == 0) word = of_last;
   }
   for (;;) {   // layers
-  for (int j = 0; j < nshare; j += 2) {
+  if constexpr (kFp4) {
+    // The tokens of a tile that count, a bit each.
+    auto seen_of = [](int meta) { return kSpan ? (uint32_t)meta >> 16 : (1u << (meta & 0xff)) - 1; };
+    while (now.j < nshare) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (now.j >= nshare) break;
+        arrived_k(kbuf[i]);
+        arrived_v(vbuf[i]);
+        const auto after = next_pair<Block>(dA, dB, jbase, walk);
+        auto issue_next_k = [&](KReg (&k)[kKLoads]) {
+          issue_k(k, after.first, 0, DD::kPerTile);
+          issue_k(k, after.second, DD::kPerTile, kKLoads);
+        };
+        auto issue_next_v = [&](VReg (&v)[kVLoads]) {
+          issue_v(v, after.first);
+          issue_v(v, after.second, DD::kPerTile);
+        };
+        const struct {
+          decltype(issue_next_k)& k;
+          decltype(issue_next_v)& v;
+        } next = {issue_next_k, issue_next_v};
+        take_q(now.first.meta);
+        if (!kWhole && (then.first.meta & kMetaSegFirst)) load_q(then.seg);
+        consume(kbuf[i], vbuf[i], now.first.meta | now.second.meta, seen_of(now.first.meta) | seen_of(now.second.meta) << 16, next);
+        now = then;
+        then = after;
+      }
+      if (!kWhole && !walk.described) {   // window A has just been begun: the one after it is described now
+        walk.described = true;
+        if (jbase + kWindow < nshare) dB = describe(jbase + kWindow);
+        else dB = Window{0, 0, 0};
+      }
+    }
+  }
+  else for (int j = 0; j < nshare; j += 2) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       KReg (&k)[kKLoads] = kbuf[i], (&knext)[kKLoads] = kbuf[i ^ 1];
