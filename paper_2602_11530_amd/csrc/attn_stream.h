@@ -288,7 +288,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   // V goes out when K is there, not a block ahead, and with it some of the next block's K loads: kAhead, or all where shares are
   // short (short_at_128; AttnLayers have a workgroup for each short segment).
   constexpr bool kLate = !kFp8 && (kD == 128 || (kD == 256 && kLarge));
-  constexpr bool kWhole = std::is_base_of_v<WholeLayer, Layers>;
+  constexpr bool kWhole = std::is_base_of_v<GroupPerSegment, Layers>;
   constexpr int kNextK = kD == 128 && (!kLarge || std::is_same_v<Layers, AttnLayers>) ? kKLoads : kAhead;
   // the next block's loads go out before this one's have arrived
   constexpr bool kTwoBlocks = !kFp4 && kD == 64 && kFp8;
@@ -418,13 +418,13 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     load_q(s * Hkv + blockIdx.x);
     typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
     whole_len = min(max(*(ScalarLoad)(a.context_lens + s), 0), a.max_ctx);
-    const int nb = (whole_len + kBlockTokens - 1) / kBlockTokens;
+    const int nb = kSpan ? units_of(whole_len) : (whole_len + kBlockTokens - 1) / kBlockTokens;
     if (nb == 0) {   // an empty request owes zero rows
       uint32_t* dst = (uint32_t*)(layer.out + (int64_t)seg_next * G * kD);
       for (int f = threadIdx.x; f < G * kD / 2; f += kThreads) dst[f] = 0;
       return;
     }
-    if (lane * a.upb < nb) whole_entry = a.block_tables[(int64_t)s * a.MAXB + lane];   // entries behind the last block are never read
+    if (!kSpan && lane * a.upb < nb) whole_entry = a.block_tables[(int64_t)s * a.MAXB + lane];   // entries behind the last block are never read
     W = min(kGroupWaves, nb);
     last_wave = W - 1;
     if (wave < W) {
@@ -533,6 +533,22 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   // The blocks of a wavefront that has its part of one segment: all in one window, their table entries in the lanes' hands.
   auto describe_whole = [&]() -> Window {
     const bool live = lane < nshare;
+    if constexpr (kSpan) {   // the blocks need not be in a row: each lane has its own block's entry
+      const int b = pos0 + lane, u = layers.span.unit(b, whole_len), tb = u >> upb_bits;
+      const int id = live ? a.block_tables[(int64_t)blockIdx.z * a.MAXB + tb] : -1;
+      const bool mapped = (unsigned)id < (unsigned)a.NB;
+      refused += __popcll(__ballot(live && !mapped));
+      const bool ends = b + 1 == units_of(whole_len);
+      const bool last = ends || ((b + 1) % bpp == 0) || (lane + 1 == nshare);
+      Window d;
+      d.slab = mapped ? (((id * Hkv + (int)blockIdx.x) << upb_bits) + (u - (tb << upb_bits))) : 0;
+      d.meta = !live ? 0
+                     : (mapped ? min(kBlockTokens, whole_len - kBlockTokens * u) : 0) | (last ? kMetaLast : 0) |
+                           (lane == 0 ? kMetaSegFirst : 0) | (ends ? kMetaSegEnd : 0) | (pos0 > 0 ? kMetaOpenLeft : 0) |
+                           (int)((mapped ? layers.span.seen(u, whole_len) : 0u) << 16);
+      d.seg = seg_next;
+      return d;
+    }
     const int b = pos0 + lane, tb = b >> upb_bits;
     const int id = __shfl(whole_entry, tb);   // by all lanes: the entries are in lanes that may have no block
     const bool mapped = live && (unsigned)id < (unsigned)a.NB;

@@ -22,6 +22,7 @@ hipError_t launch_attn_span(const AttnLaunch& a_in, const Span* span, hipStream_
   a.wave_lds_floats = l.wave;
   a.turns = !fp4 && l.turn_bytes > 0;
   const size_t lds = l.bytes + (fp4 ? 0 : l.turn_bytes);
+  if (!a.leaves_records) return launch_attn_span_whole(a, span, lds, stream);
   if (fp4) return launch_attn_fp4(a, span, lds, stream);
   SpanLayer layer;
   layer.span = *span;

@@ -177,7 +177,8 @@ struct AttnLayers {
   AttnLayer layer[kMaxLaunchLayers];
 };
 struct OneLayer {};
-struct WholeLayer : OneLayer {};   // a workgroup for each segment
+struct GroupPerSegment {};   // a workgroup for each segment
+struct WholeLayer : OneLayer, GroupPerSegment {};
 // Which tokens a request of L sees: its last `window`, and its first `sinks`.  Both are at most the longest context.  Of its 16-token units
 // those that hold such a token are attended over, in order; what lies between the sinks and the window is no part of the stream.
 struct Span {
@@ -213,6 +214,9 @@ struct SpanLayer : OneLayer {
 struct Fp4Pools {};
 struct Fp4Layer : OneLayer, Fp4Pools {};
 struct Fp4SpanLayer : SpanLayer, Fp4Pools {};
+struct WholeSpanLayer : SpanLayer, GroupPerSegment {};
+struct WholeFp4Layer : Fp4Layer, GroupPerSegment {};
+struct WholeFp4SpanLayer : Fp4SpanLayer, GroupPerSegment {};
 // One after the other in each workgroup.
 struct ChainedLayers : AttnLayers {};
 __device__ __forceinline__ int layer_index(const OneLayer&) { return 0; }
@@ -294,7 +298,9 @@ inline bool short_at_128(const AttnLaunch& a) {
 }
 // The stream pass over E2M1 tiles, or for requests that see part of their context, or both.  `span`: nullptr for all of it.
 hipError_t launch_attn_span(const AttnLaunch& a, const Span* span, hipStream_t stream);
-hipError_t launch_attn_fp4(const AttnLaunch& a, const Span* span, size_t lds, hipStream_t stream);   // with LDS laid out
+// With LDS laid out: over tiles, and where each segment has a workgroup.
+hipError_t launch_attn_fp4(const AttnLaunch& a, const Span* span, size_t lds, hipStream_t stream);
+hipError_t launch_attn_span_whole(const AttnLaunch& a, const Span* span, size_t lds, hipStream_t stream);
 // The stream pass's kernels for one layer of those, and for layers one after the other.
 void launch_large_256(const AttnLaunch& a, size_t lds, hipStream_t stream);
 void launch_short_128(const AttnLaunch& a, size_t lds, hipStream_t stream);
