@@ -412,6 +412,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     }
   }
   // What lies where each segment has a workgroup.
+  constexpr bool kOwnEntry = kSpan || kFp4;
   int whole_len = 0, whole_entry = 0;
   if constexpr (kWhole) {
     const int s = blockIdx.z;
@@ -424,7 +425,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       for (int f = threadIdx.x; f < G * kD / 2; f += kThreads) dst[f] = 0;
       return;
     }
-    if (!kSpan && lane * a.upb < nb) whole_entry = a.block_tables[(int64_t)s * a.MAXB + lane];   // entries behind the last block are never read
+    if (!kOwnEntry && lane * a.upb < nb) whole_entry = a.block_tables[(int64_t)s * a.MAXB + lane];   // entries behind the last block are never read
     W = min(kGroupWaves, nb);
     last_wave = W - 1;
     if (wave < W) {
@@ -533,8 +534,11 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   // The blocks of a wavefront that has its part of one segment: all in one window, their table entries in the lanes' hands.
   auto describe_whole = [&]() -> Window {
     const bool live = lane < nshare;
-    if constexpr (kSpan) {   // the blocks need not be in a row: each lane has its own block's entry
-      const int b = pos0 + lane, u = layers.span.unit(b, whole_len), tb = u >> upb_bits;
+    if constexpr (kOwnEntry) {   // the blocks need not be in a row, or are many: each lane has its own block's entry
+      const int b = pos0 + lane;
+      int u = b;   // unit of the request
+      if constexpr (kSpan) u = layers.span.unit(b, whole_len);
+      const int tb = u >> upb_bits;
       const int id = live ? a.block_tables[(int64_t)blockIdx.z * a.MAXB + tb] : -1;
       const bool mapped = (unsigned)id < (unsigned)a.NB;
       refused += __popcll(__ballot(live && !mapped));
@@ -544,8 +548,8 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       d.slab = mapped ? (((id * Hkv + (int)blockIdx.x) << upb_bits) + (u - (tb << upb_bits))) : 0;
       d.meta = !live ? 0
                      : (mapped ? min(kBlockTokens, whole_len - kBlockTokens * u) : 0) | (last ? kMetaLast : 0) |
-                           (lane == 0 ? kMetaSegFirst : 0) | (ends ? kMetaSegEnd : 0) | (pos0 > 0 ? kMetaOpenLeft : 0) |
-                           (int)((mapped ? layers.span.seen(u, whole_len) : 0u) << 16);
+                           (lane == 0 ? kMetaSegFirst : 0) | (ends ? kMetaSegEnd : 0) | (pos0 > 0 ? kMetaOpenLeft : 0);
+      if constexpr (kSpan) d.meta |= (int)((mapped ? layers.span.seen(u, whole_len) : 0u) << 16);
       d.seg = seg_next;
       return d;
     }

@@ -91,6 +91,14 @@ inline int short_segment(int64_t segments, int D, bool kv_fp8) {
   return (segments <= 64 && block_bytes >= 8192 ? 3 : 6) * group_waves(D);
 }
 
+// The same for tiles, which are half as large again or less.  Up to 12 blocks per wavefront where most compute units have a segment, else as
+// above.  Us for append and attention at 3 or 6 blocks, 12, 24: 256 segments of 800..1536 tokens 21.2 / 18.0 / 17.5, at D = 64 18.0 / 14.6,
+// at D = 256 of 400..768 23.3 / 18.7; 128 of 800..1536 17.5 / 16.4 / 16.5, of 1500..3000 20.9 / 21.1 / 23.9; 256 of those 25.7 / 26.1 / 25.5;
+// 8 segments of 900..1536 13.8 / 15.3, at D = 64 13.6 / 13.2.
+inline int short_segment_fp4(int64_t segments, int D) {
+  return segments <= 64 ? short_segment(segments, D, true) : 12 * group_waves(D);
+}
+
 // A segment that several workgroups share, as those of them leave it in which no later one begins: the one that it begins in and
 // those in its middle.
 struct SharedSegment {
