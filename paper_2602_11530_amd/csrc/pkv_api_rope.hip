@@ -17,6 +17,9 @@ Range rows_at(const void* p, int64_t tokens, int64_t stride, int64_t width) {
 }
 bool meet(const Range& x, const Range& y) { return x.from < y.to && y.from < x.to; }
 
+// Quotients that are not beyond the format's range nor round to zero in it, and their remainders, are normal numbers.
+float inverse_of(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f ? 1.f / scale : 0.f; }
+
 constexpr int64_t kMaxTokens = ((int64_t)1 << 24) - 1;   // a workgroup of 256 lanes for each in one dimension of a launch
 constexpr int64_t kMaxStride = (int64_t)1 << 31;
 
@@ -75,6 +78,8 @@ int rope_append(const void* q, const void* k, const void* v, const void* q_norm,
   a.eps = rope->norm_eps;
   a.k_scale = k_scale;
   a.v_scale = v_scale;
+  a.k_inverse = inverse_of(k_scale);
+  a.v_inverse = inverse_of(v_scale);
   a.kv_fp8 = kv_fp8;
   a.T = (int)T;
   a.S = shape->num_seqs;

@@ -91,7 +91,7 @@ inline int short_segment(int64_t segments, int D, bool kv_fp8) {
   return (segments <= 64 && block_bytes >= 8192 ? 3 : 6) * group_waves(D);
 }
 
-// The same for tiles, which are half as large again or less.  Up to 12 blocks per wavefront where most compute units have a segment, else as
+// The same for tiles, a little more than half of what e4m3 takes.  Up to 12 blocks per wavefront where most compute units have a segment, else as
 // above.  Us for append and attention at 3 or 6 blocks, 12, 24: 256 segments of 800..1536 tokens 21.2 / 18.0 / 17.5, at D = 64 18.0 / 14.6,
 // at D = 256 of 400..768 23.3 / 18.7; 128 of 800..1536 17.5 / 16.4 / 16.5, of 1500..3000 20.9 / 21.1 / 23.9; 256 of those 25.7 / 26.1 / 25.5;
 // 8 segments of 900..1536 13.8 / 15.3, at D = 64 13.6 / 13.2.
@@ -374,6 +374,7 @@ struct RopeLaunch {
   const int32_t* token_starts;           // [S + 1]; nullptr: token s is request s's last one
   int32_t* id_faults;
   float eps, k_scale, v_scale;
+  float k_inverse, v_inverse;            // their reciprocals, 0 where a remainder might leave fp32's range
   int kv_fp8;                            // as in AttnLaunch
   int T, S, Hq, Hkv, D, R, interleaved;
   int MAXB, log_block, max_ctx, NB;
