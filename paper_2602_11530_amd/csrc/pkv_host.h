@@ -114,7 +114,7 @@ inline int prepare_attn(const int32_t* block_tables, const int32_t* context_lens
   const int64_t max_blocks = span ? span->most_units(g.max_ctx) : (g.max_ctx + kBlockTokens - 1) / kBlockTokens;
   a->short_blocks = kv_fp8 == kFp4Pools ? short_segment_fp4(segments, a->D) : short_segment(segments, a->D, kv_fp8);
   a->leaves_records = 1;
-  if (segments <= a->waves / group && max_blocks <= a->short_blocks) {
+  if (cut_by_segment(segments, a->D, span, kv_fp8 == kFp4Pools) && max_blocks <= a->short_blocks) {
     // Cut along its segments, a workgroup for each.  Nothing is left in the workspace, and the layers of such
     // a launch may be more than it has room for.
     a->leaves_records = 0;
