@@ -5,12 +5,14 @@
 //   (a, b) -> (a cos - b sin, b cos + a sin)    pairs (j, j + R/2) or (2j, 2j + 1) of the first R dims; cos and sin from the position's row
 //
 // in fp32, rounded once to what is stored.  Prompts are bound by memory, each row in and out once (16 of 100..2000 tokens on 40/8 heads, 505 MB,
-// 94 us: 5.4 TB/s, a 1 GiB copy 4.8), a step's few tokens by the launch and three round trips: lengths, the position's row and table entry,
+// 88 us: 5.7 TB/s, a 1 GiB copy 4.8), a step's few tokens by the launch and three round trips: lengths, the position's row and table entry,
 // stores.  D / 8 lanes have a row, and a lane two pieces of four dims: with pairs (j, j + R/2) those of both
 // halves, so that a rotation stays in the lane, else (and behind the first R dims) eight in a row.  The sum of squares is all that lanes
 // exchange.
 #include "fp4.h"
 #include "pkv_kernels.h"
+
+#include <type_traits>
 
 namespace pkv {
 namespace {
@@ -36,14 +38,19 @@ __device__ __forceinline__ void unpack(const Raw& w, float (&x)[8]) {
     x[2 * i + 1] = __uint_as_float(w.piece[i >> 1][i & 1] & 0xffff0000u);
   }
 }
+// By value: a choice between members of a struct would be one between their addresses, and the struct would live in memory.
+__device__ __forceinline__ int choose(bool one, int x, int y) { return one ? x : y; }
+__device__ __forceinline__ Raw choose(bool one, Raw x, Raw y) {
+  return Raw{{one ? x.piece[0] : y.piece[0], one ? x.piece[1] : y.piece[1]}};
+}
 __device__ __forceinline__ Raw load(const uint16_t* row, int p0, int p1) { return Raw{{*(const u32x2*)(row + p0), *(const u32x2*)(row + p1)}}; }
 __device__ __forceinline__ float to_range(float y) {
   return (y != y) ? y : fminf(fmaxf(y, -448.f), 448.f);   // NaN stays NaN
 }
 
 // A lane's pieces, which begin at dims p0 and p1, into a row; nontemporal, as nothing of a prompt is read again soon: 16 prompts of 100..2000 tokens on
-// 40/8 heads 105 us with ordinary stores, 100 this way, 24 pieces of 1..900 in e4m3 at D = 64 29.5 and 24.2; nontemporal loads gain nothing and cost
-// 4 us where the projection's rows are still on chip.
+// 40/8 heads 105 us with ordinary stores, 100 this way (of an earlier kernel), 24 pieces of 1..900 in e4m3 at D = 64 29.5 and 24.2; nontemporal loads
+// gain nothing and cost 4 us where the projection's rows are still on chip.
 __device__ __forceinline__ void put_bf16(char* row, int p0, int p1, const float (&y)[8]) {
   __builtin_nontemporal_store(u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])}, (u32x2*)(row + 2 * p0));
   __builtin_nontemporal_store(u32x2{pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])}, (u32x2*)(row + 2 * p1));
@@ -99,92 +106,87 @@ __device__ __forceinline__ void put_fp4(char* tile, int t, int chunk, const floa
   if ((chunk & 3) == 0) *(uint8_t*)(tile + fp4_scale_place(kD, chunk >> 2, t)) = most > 0x7f800000u ? 255 : byte;
 }
 
-// A token's request and position (< 0: it has none).
+// A token's request and position (< 0: it has none), and how many tokens from it on are the request's.
 struct TokenAt {
-  int request, position;
+  int request, position, behind;
 };
+// `end`: where the request's tokens end; `len`: its context length.
+__device__ __forceinline__ TokenAt placed(const RopeLaunch& a, int request, int token, int end, int len) {
+  const int L = min(max(len, 0), a.max_ctx);
+  const uint32_t behind = (uint32_t)end - (uint32_t)token;
+  if (end <= token || behind > (uint32_t)L) return {0, -1, 1};
+  return {request, (int)((uint32_t)L - behind), (int)behind};
+}
+// For all lanes the same.
 __device__ __forceinline__ TokenAt token_at(const RopeLaunch& a, int token) {
   typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
-  int s = token, len;
-  uint32_t behind = 1;   // tokens of the request from this one on
-  if (a.token_starts) {
-    // The last request that begins at or before the token: one look of 64 lanes up to 63 requests, else two, kMaxSeqs being 32 times 64.  Its
-    // length and where the next one begins come with the last look.
-    const int lane = threadIdx.x & 63, step = (a.S >> 6) + 1;
-    int base = 0;
-    if (step > 1) {
-      const int i = lane * step;
-      const int begin = i < a.S ? a.token_starts[i] : INT32_MAX;
-      base = max(__popcll(__ballot(begin <= token)) - 1, 0) * step;
-    }
-    const int j = base + lane;
-    const int at = j <= a.S ? a.token_starts[j] : INT32_MAX, length = j < a.S ? a.context_lens[j] : 0;
-    const int found = __popcll(__ballot(j < a.S && lane < 63 && at <= token)) - 1;
-    if (found < 0) return {0, -1};
-    const int end = __builtin_amdgcn_readlane(at, found + 1);
-    if (end <= token) return {0, -1};
-    s = base + found;
-    len = __builtin_amdgcn_readlane(length, found);
-    behind = (uint32_t)end - (uint32_t)token;
-  } else {
-    len = *(ScalarLoad)(a.context_lens + s);
+  if (!a.token_starts) return placed(a, token, token, token + 1, *(ScalarLoad)(a.context_lens + token));
+  // The last request that begins at or before the token: one look of 64 lanes up to 63 requests, else two, kMaxSeqs being 32 times 64.  Its
+  // length and where the next one begins come with the last look.
+  const int lane = threadIdx.x & 63, step = (a.S >> 6) + 1;
+  int base = 0;
+  if (step > 1) {
+    const int i = lane * step;
+    const int begin = i < a.S ? a.token_starts[i] : INT32_MAX;
+    base = max(__popcll(__ballot(begin <= token)) - 1, 0) * step;
   }
-  const int L = min(max(len, 0), a.max_ctx);
-  const int position = (int)((uint32_t)L - behind);
-  return {s, behind <= (uint32_t)L ? position : -1};
+  const int j = base + lane;
+  const int at = j <= a.S ? a.token_starts[j] : INT32_MAX, length = j < a.S ? a.context_lens[j] : 0;
+  const int found = __popcll(__ballot(j < a.S && lane < 63 && at <= token)) - 1;
+  if (found < 0) return {0, -1, 1};
+  return placed(a, base + found, token, __builtin_amdgcn_readlane(at, found + 1), __builtin_amdgcn_readlane(length, found));
+}
+// Each lane's own.
+__device__ __forceinline__ TokenAt lane_token_at(const RopeLaunch& a, int token) {
+  if (!a.token_starts) return placed(a, token, token, token + 1, a.context_lens[token]);
+  int s = -1;   // the last request that begins at or before the token
+  for (int step = 1 << (31 - __clz(a.S)); step > 0; step >>= 1)
+    if (s + step < a.S && a.token_starts[s + step] <= token) s += step;
+  if (s < 0) return {0, -1, 1};
+  return placed(a, s, token, a.token_starts[s + 1], a.context_lens[s]);
 }
 
-// A workgroup has kPasses times kRows rows of a token.  They are all asked for before its position is looked up.
-template <int kD, int kFormat, int kPasses>
-__global__ __launch_bounds__(kThreads) void kv_rope_kernel(RopeLaunch a) {
-  constexpr bool kFp4 = kFormat == kFp4Pools;
-  constexpr int kLanes = kD / 8;            // of a row
-  constexpr int kRows = kThreads / kLanes;  // at a time
-  const int token = blockIdx.x;
-  const int n = threadIdx.x & (kLanes - 1);
-  const int rows = a.Hq + 2 * a.Hkv;
-  const int row0 = blockIdx.y * kPasses * kRows + threadIdx.x / kLanes;
-
-  // Where a lane's pieces begin: in a query or key, and in a value.  Tiles want eight dims in a row.
-  const int half = a.R >> 1, split = a.R || kFp4 ? half : kD / 2;
-  const bool turned = 8 * n < a.R, apart = !a.interleaved && 4 * n < split;
-  const int p0 = apart ? 4 * n : 8 * n, p1 = apart ? split + 4 * n : 8 * n + 4;
-  const int v0 = kFp4 ? 8 * n : 4 * n, v1 = kFp4 ? 8 * n + 4 : kD / 2 + 4 * n;
-  Raw raw[kPasses];
-  const uint16_t* const q = a.q + token * a.q_stride;
-  const uint16_t* const k = a.k + token * a.k_stride - a.Hq * kD;
-  const uint16_t* const v = a.v + token * a.v_stride - (a.Hq + a.Hkv) * kD;
-#pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    const int r = min(row0 + i * kRows, rows - 1);
-    const bool is_v = r >= a.Hq + a.Hkv;
-    raw[i] = load((is_v ? v : r >= a.Hq ? k : q) + r * kD, is_v ? v0 : p0, is_v ? v1 : p1);
+// What is a lane's of the rows it has: its pieces begin at p0 and p1 in a query or key, at v0 and v1 in a value (tiles want eight dims in a row).
+template <int kD, int kFormat>
+struct Lane {
+  static constexpr bool kFp4 = kFormat == kFp4Pools;
+  static constexpr int kLanes = kD / 8;             // of a row
+  static constexpr int kRows = kThreads / kLanes;   // of a workgroup, at a time
+  int n, half, p0, p1, v0, v1;
+  bool turned;
+  Raw q_norm, k_norm;
+  __device__ __forceinline__ Lane(const RopeLaunch& a) {
+    n = threadIdx.x & (kLanes - 1);
+    half = a.R >> 1;
+    turned = 8 * n < a.R;
+    const int split = a.R || kFp4 ? half : kD / 2;
+    const bool apart = !a.interleaved && 4 * n < split;
+    p0 = apart ? 4 * n : 8 * n;
+    p1 = apart ? split + 4 * n : 8 * n + 4;
+    v0 = kFp4 ? 8 * n : 4 * n;
+    v1 = kFp4 ? 8 * n + 4 : kD / 2 + 4 * n;
+    q_norm = k_norm = Raw{};
+    if (a.q_norm) q_norm = load(a.q_norm, p0, p1);
+    if (a.k_norm) k_norm = load(a.k_norm, p0, p1);
   }
-  Raw q_norm = {}, k_norm = {};
-  if (a.q_norm) q_norm = load(a.q_norm, p0, p1);
-  if (a.k_norm) k_norm = load(a.k_norm, p0, p1);
-
-  const TokenAt at = token_at(a, token);
-  if (at.position < 0) return;
-  f32x4 cs = {}, sn = {};
-  if (turned) {
-    const float* row = a.cos_sin + (int64_t)at.position * a.R + 4 * n;
+  // Row r of a token: its queries, its keys, its values.
+  __device__ __forceinline__ Raw ask(const RopeLaunch& a, int64_t token, int r) const {
+    const bool is_v = r >= a.Hq + a.Hkv;
+    const uint16_t* row = is_v ? a.v + token * a.v_stride - (a.Hq + a.Hkv) * kD : r >= a.Hq ? a.k + token * a.k_stride - a.Hq * kD : a.q + token * a.q_stride;
+    return load(row + r * kD, choose(is_v, v0, p0), choose(is_v, v1, p1));
+  }
+  __device__ __forceinline__ void ask_turn(const RopeLaunch& a, int position, f32x4& cs, f32x4& sn) const {
+    if (!turned) return;
+    const float* row = a.cos_sin + (int64_t)position * a.R + 4 * n;
     cs = *(const f32x4*)row;
     sn = *(const f32x4*)(row + half);
   }
-  const int id = a.block_tables[(int64_t)at.request * a.MAXB + (at.position >> a.log_block)];
-  const bool mapped = (unsigned)id < (unsigned)a.NB;   // never follow a corrupt id; report it once per token
-  if (!mapped && a.id_faults && blockIdx.y == 0 && threadIdx.x == 0) atomicAdd(a.id_faults, 1);
-  const int slot = at.position & ((1 << a.log_block) - 1);
-
-#pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    __builtin_amdgcn_sched_barrier(0);   // one after the other: all at once takes three times the registers, and the workgroups on a unit hide the rest
-    const int r = row0 + i * kRows;
-    if (r >= rows) break;
+  // A row that has arrived, to where it belongs; `id`: the block of its position.
+  __device__ __forceinline__ void finish(const RopeLaunch& a, int64_t token, int r, int position, int id, const Raw& raw, const f32x4& cs,
+                                         const f32x4& sn) const {
     const bool is_q = r < a.Hq, is_v = r >= a.Hq + a.Hkv;
     float x[8];
-    unpack(raw[i], x);
+    unpack(raw, x);
     if (!is_v) {
       if (is_q ? a.q_norm : a.k_norm) {
         float sum = 0.f;
@@ -194,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void kv_rope_kernel(RopeLaunch a) {
         for (int m = 1; m < kLanes; m <<= 1) sum += __shfl_xor(sum, m);
         const float inv = __builtin_amdgcn_rsqf(sum * (1.f / kD) + a.eps);   // within a unit in the last place
         float w[8];
-        unpack(is_q ? q_norm : k_norm, w);
+        unpack(choose(is_q, q_norm, k_norm), w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * w[e];
       }
@@ -216,58 +218,143 @@ __global__ __launch_bounds__(kThreads) void kv_rope_kernel(RopeLaunch a) {
       }
     }
     if (is_q) {
-      put_bf16((char*)(a.q_out + ((int64_t)token * a.Hq + r) * kD), p0, p1, x);
-    } else if (mapped) {
-      const int head = is_v ? r - a.Hq - a.Hkv : r - a.Hq;
-      const int64_t units = ((int64_t)id * a.Hkv + head) << (a.log_block - 4);
-      char* pool = (char*)(is_v ? a.v_pool : a.k_pool);
-      if constexpr (kFp4) {
-        if (!is_v && half && !a.interleaved) {
-          // the pieces that hold this lane's eight dims in a row, out of the lanes that have them
-          float y[8];
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const int d = 8 * n + 4 * z;
-            const bool low = d < half, high = !low && d < a.R;
-            const int from = low ? d >> 2 : high ? (d - half) >> 2 : n;
-            const bool second = high || (!low && z == 1);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float one = __shfl(x[e], from, kLanes), two = __shfl(x[4 + e], from, kLanes);
-              y[4 * z + e] = second ? two : one;
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = y[e];
-        }
-        put_fp4<kD>(pool + (units + (slot >> 4)) * fp4_tile_bytes(kD), slot & 15, n, x, is_v);
-      } else if constexpr (kFormat == 1) {
-        char* row = pool + (units * kBlockTokens + slot) * kD;
-        put_fp8(row, is_v ? v0 : p0, is_v ? v1 : p1, x, is_v ? a.v_scale : a.k_scale, is_v ? a.v_inverse : a.k_inverse);
-      } else {
-        put_bf16(pool + (units * kBlockTokens + slot) * kD * 2, is_v ? v0 : p0, is_v ? v1 : p1, x);
-      }
+      put_bf16((char*)(a.q_out + (token * a.Hq + r) * kD), p0, p1, x);
+      return;
     }
+    if ((unsigned)id >= (unsigned)a.NB) return;   // never follow a corrupt id
+    const int slot = position & ((1 << a.log_block) - 1), head = is_v ? r - a.Hq - a.Hkv : r - a.Hq;
+    const int64_t units = ((int64_t)id * a.Hkv + head) << (a.log_block - 4);
+    char* pool = (char*)(is_v ? a.v_pool : a.k_pool);
+    if constexpr (kFp4) {
+      if (!is_v && half && !a.interleaved) {
+        // the pieces that hold this lane's eight dims in a row, out of the lanes that have them
+        float y[8];
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const int d = 8 * n + 4 * z;
+          const bool low = d < half, high = !low && d < a.R;
+          const int from = low ? d >> 2 : high ? (d - half) >> 2 : n;
+          const bool second = high || (!low && z == 1);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float one = __shfl(x[e], from, kLanes), two = __shfl(x[4 + e], from, kLanes);
+            y[4 * z + e] = second ? two : one;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = y[e];
+      }
+      put_fp4<kD>(pool + (units + (slot >> 4)) * fp4_tile_bytes(kD), slot & 15, n, x, is_v);
+    } else if constexpr (kFormat == 1) {
+      char* row = pool + (units * kBlockTokens + slot) * kD;
+      put_fp8(row, choose(is_v, v0, p0), choose(is_v, v1, p1), x, is_v ? a.v_scale : a.k_scale, is_v ? a.v_inverse : a.k_inverse);
+    } else {
+      put_bf16(pool + (units * kBlockTokens + slot) * kD * 2, choose(is_v, v0, p0), choose(is_v, v1, p1), x);
+    }
+  }
+};
+
+// Reports a refused id, once per token.
+__device__ __forceinline__ void report(const RopeLaunch& a, int id) {
+  if ((unsigned)id >= (unsigned)a.NB && a.id_faults) atomicAdd(a.id_faults, 1);
+}
+
+// A workgroup has kPasses times kRows rows of a token.  They are all asked for before its position is looked up.
+template <int kD, int kFormat, int kPasses>
+__global__ __launch_bounds__(kThreads) void kv_rope_kernel(RopeLaunch a) {
+  typedef Lane<kD, kFormat> L;
+  const int token = blockIdx.x, rows = a.Hq + 2 * a.Hkv;
+  const int row0 = blockIdx.y * kPasses * L::kRows + threadIdx.x / L::kLanes;
+  const L lane(a);
+  Raw raw[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) raw[i] = lane.ask(a, token, min(row0 + i * L::kRows, rows - 1));
+  asm volatile("" : : : "memory");   // all of them go out here, none only where it is used
+  const TokenAt at = token_at(a, token);
+  if (at.position < 0) return;
+  f32x4 cs = {}, sn = {};
+  lane.ask_turn(a, at.position, cs, sn);
+  const int id = a.block_tables[(int64_t)at.request * a.MAXB + (at.position >> a.log_block)];
+  if (blockIdx.y == 0 && threadIdx.x == 0) report(a, id);
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    __builtin_amdgcn_sched_barrier(0);   // one after the other: all at once takes three times the registers, and the workgroups on a unit hide the rest
+    const int r = row0 + i * L::kRows;
+    if (r >= rows) break;
+    lane.finish(a, token, r, at.position, id, raw[i], cs, sn);
   }
 }
 
-template <int kD, int kPasses>
+// The rows of all tokens one after the other, where a token has few: a workgroup has kPasses times kRows of them, of several tokens.
+template <int kD, int kFormat, int kPasses>
+__global__ __launch_bounds__(kThreads) void kv_rope_rows_kernel(RopeLaunch a) {
+  typedef Lane<kD, kFormat> L;
+  const int rows = a.Hq + 2 * a.Hkv;
+  const uint32_t from = blockIdx.x * (uint32_t)(kPasses * L::kRows);   // below T * rows, which is less than 2^24 * 32
+  const int first = from / (uint32_t)rows, ahead = from - (uint32_t)first * rows;   // the first token, and its rows that others have
+  const float per = __builtin_amdgcn_rcpf((float)rows);
+  const L lane(a);
+  Raw raw[kPasses];
+  int token[kPasses], row[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int at = ahead + i * L::kRows + threadIdx.x / L::kLanes;
+    const int t = (int)(((float)at + 0.5f) * per);   // a small quotient: (x + 1/2) / n is 1 / (2n) away from a whole number
+    row[i] = at - t * rows;
+    token[i] = first + t;
+    raw[i] = lane.ask(a, min(token[i], a.T - 1), row[i]);
+  }
+  asm volatile("" : : : "memory");   // all of them go out here, none only where it is used
+  const TokenAt begin = token_at(a, first);
+  int position[kPasses], id[kPasses];
+  f32x4 cs[kPasses] = {}, sn[kPasses] = {};
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    TokenAt at = begin;
+    const int d = token[i] - first;
+    if (d < begin.behind) at.position += d;
+    else at = lane_token_at(a, min(token[i], a.T - 1));
+    position[i] = token[i] < a.T && at.position >= 0 ? at.position : -1;
+    id[i] = 0;
+    if (position[i] >= 0) {
+      id[i] = a.block_tables[(int64_t)at.request * a.MAXB + (position[i] >> a.log_block)];
+      lane.ask_turn(a, position[i], cs[i], sn[i]);
+    }
+  }
+  asm volatile("" : : : "memory");
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (position[i] < 0) continue;
+    if (row[i] == 0 && lane.n == 0) report(a, id[i]);
+    lane.finish(a, token[i], row[i], position[i], id[i], raw[i], cs[i], sn[i]);
+  }
+}
+
+template <int kD, int kPasses, bool kTokens>
 void launch_passes(const RopeLaunch& a, hipStream_t stream) {
   constexpr int kRows = kPasses * (kThreads / (kD / 8));
-  const dim3 grid(a.T, (a.Hq + 2 * a.Hkv + kRows - 1) / kRows);
-  if (a.kv_fp8 == kFp4Pools) hipLaunchKernelGGL((kv_rope_kernel<kD, kFp4Pools, kPasses>), grid, dim3(kThreads), 0, stream, a);
-  else if (a.kv_fp8) hipLaunchKernelGGL((kv_rope_kernel<kD, 1, kPasses>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((kv_rope_kernel<kD, 0, kPasses>), grid, dim3(kThreads), 0, stream, a);
+  const int rows = a.Hq + 2 * a.Hkv;
+  const dim3 grid = kTokens ? dim3(a.T, (rows + kRows - 1) / kRows) : dim3((unsigned)(((int64_t)a.T * rows + kRows - 1) / kRows));
+  const auto kernel = [&](auto format) {
+    if constexpr (kTokens) return kv_rope_kernel<kD, decltype(format)::value, kPasses>;
+    else return kv_rope_rows_kernel<kD, decltype(format)::value, kPasses>;
+  };
+  const auto k = a.kv_fp8 == kFp4Pools ? kernel(std::integral_constant<int, kFp4Pools>{})
+                 : a.kv_fp8            ? kernel(std::integral_constant<int, 1>{})
+                                       : kernel(std::integral_constant<int, 0>{});
+  hipLaunchKernelGGL(k, grid, dim3(kThreads), 0, stream, a);
 }
-// Few tokens: as many workgroups as their rows give.  Many: up to four rows a lane, for which a position is looked up once (us at one, two and
-// four, the kernel before lanes had both halves of a rotation: 16 prompts of 100..2000 tokens on 40/8 heads 142 / 113 / 105, at D = 256 256 / 218 / 200;
-// 24 pieces of 1..900 in e4m3 on 32/8 heads at D = 64, of which two are all, 32 / 27).
+// Few tokens: as many workgroups as their rows give.  Many: up to four rows a lane, for which a position is looked up once; where a token's rows
+// do not fill a workgroup, rows of several tokens.  Us for 16 prompts of 100..2000 tokens: 40/8 heads 88, the rows in a row 111, at D = 256 176 /
+// 208, 28/4 heads 66 / 72; 8/2 heads 27.8 / 23.7, 8/1 26.8 / 21.0, at D = 64 23.2 / 12.1, 16/8 there 30.5 / 28.6.
 template <int kD>
 void launch_dim(const RopeLaunch& a, hipStream_t stream) {
   const int rows = a.Hq + 2 * a.Hkv, at_a_time = kThreads / (kD / 8);
-  if (a.T < 1024 || rows <= at_a_time) launch_passes<kD, 1>(a, stream);
-  else if (rows <= 2 * at_a_time) launch_passes<kD, 2>(a, stream);
-  else launch_passes<kD, 4>(a, stream);
+  if (a.T < 1024) launch_passes<kD, 1, true>(a, stream);
+  else if (rows <= at_a_time) launch_passes<kD, 2, false>(a, stream);
+  else if (rows <= 2 * at_a_time) launch_passes<kD, 2, true>(a, stream);
+  else launch_passes<kD, 4, true>(a, stream);
 }
 
 }  // namespace

@@ -101,7 +101,7 @@ def test_attention(device, dim, block, hq, hkv):
 
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
-@pytest.mark.parametrize("seqs,hkv,longest", [(70, 2, 300), (300, 1, 120), (1, 8, 8191), (2048, 1, 20)])
+@pytest.mark.parametrize("seqs,hkv,longest", [(70, 2, 300), (300, 1, 120), (90, 2, 1500), (230, 2, 900), (1, 8, 8191), (2048, 1, 20)])
 def test_attention_of_many_requests_and_long_ones(device, dim, seqs, hkv, longest):
     rng = np.random.default_rng(seqs)
     lens = rng.integers(0, longest + 1, seqs)

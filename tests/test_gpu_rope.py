@@ -211,6 +211,37 @@ def test_requests_are_found(device, seqs):
     check(b, pools, run(b, pools, starts_of(new)))
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim,hq,hkv", [(64, 8, 1), (64, 16, 8), (64, 20, 5), (128, 3, 1), (128, 8, 8), (128, 40, 8), (256, 2, 1), (256, 10, 5)])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_many_tokens(device, kind, dim, hq, hkv, ragged):
+    """From 1024 tokens on: rows of several tokens to a workgroup, or several of a token to a lane; with padding, requests with none and ones
+    with more tokens than context."""
+    rng = np.random.default_rng(dim + hq)
+    if ragged:
+        new = np.array([0, 700, 1, 0, 0, 333, 40, 2, 60])
+        lens = new + np.array([3, 0, 17, 0, 5, 1, -30, 0, 100])       # request 6 has ten tokens of context
+        b = make_batch(lens, hq, hkv, dim, 16, seed=52, spare=2)
+        pools = pools_of(b, kind)
+        check(b, pools, run(b, pools, 2 + starts_of(new), tokens=1151))
+    else:
+        b = make_batch(rng.integers(0, 40, 1100), hq, hkv, dim, 16, seed=53)
+        pools = pools_of(b, kind)
+        check(b, pools, run(b, pools))
+
+
+@pytest.mark.expects_id_faults
+def test_many_tokens_with_ids_outside_the_pool(device, id_faults):
+    b = make_batch(np.full(40, 30), 3, 1, 64, 16, seed=54, spare=1)
+    pools = pools_of(b, "bf16")
+    right = b.tables.copy()
+    b.tables[7, 1] = b.num_blocks                                # tokens 16..29 of request 7
+    r = run(b, pools, starts_of([30] * 40))
+    b.tables = right
+    check(b, pools, r, faulty=range(7 * 30 + 16, 8 * 30))
+    assert int(id_faults.item()) == 14
+
+
 @pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** -20, 2.0 ** 40])
 def test_small_and_large_rows(device, scale):
     """Squares that leave fp32's range give what fp32 gives, so scales stay within its root; a row of zeros stays zeros."""
