@@ -10,6 +10,7 @@ or with one that is not for this interpreter, every call goes by ctypes.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional
 
@@ -283,6 +284,14 @@ def paged_decode_attn_fp8kv(q, k_pool, v_pool, block_tables, context_lens, scale
         _check(status)
 
 
+def _int32(x) -> int:
+    """A number of tokens as the C functions take it; ctypes would keep the lower bits of a larger one."""
+    x = operator.index(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        _check(PKV_ERR_SHAPE)
+    return x
+
+
 def _ws_bytes(workspace) -> int:
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
@@ -307,7 +316,7 @@ def paged_decode_attn_window(q, k_pool, v_pool, block_tables, context_lens, scal
                                                            out, shape, workspace, stream)
     if status is NotImplemented:
         status = lib().paged_decode_attn_window(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(context_lens),
-                                                ctypes.c_float(scale), window, sinks, _ptr(out), ctypes.byref(shape),
+                                                ctypes.c_float(scale), _int32(window), _int32(sinks), _ptr(out), ctypes.byref(shape),
                                                 _ptr(workspace), _ws_bytes(workspace), _stream(stream))
     if status:
         _check(status)
@@ -321,7 +330,7 @@ def paged_decode_attn_window_fp8kv(q, k_pool, v_pool, block_tables, context_lens
     if status is NotImplemented:
         status = lib().paged_decode_attn_window_fp8kv(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
                                                       _ptr(context_lens), ctypes.c_float(scale), ctypes.c_float(k_scale),
-                                                      ctypes.c_float(v_scale), window, sinks, _ptr(out), ctypes.byref(shape),
+                                                      ctypes.c_float(v_scale), _int32(window), _int32(sinks), _ptr(out), ctypes.byref(shape),
                                                       _ptr(workspace), _ws_bytes(workspace), _stream(stream))
     if status:
         _check(status)
@@ -334,7 +343,7 @@ def paged_decode_attn_window_fp4kv(q, k_pool, v_pool, block_tables, context_lens
                                                                  sinks, out, shape, workspace, stream)
     if status is NotImplemented:
         status = lib().paged_decode_attn_window_fp4kv(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables),
-                                                      _ptr(context_lens), ctypes.c_float(scale), window, sinks, _ptr(out),
+                                                      _ptr(context_lens), ctypes.c_float(scale), _int32(window), _int32(sinks), _ptr(out),
                                                       ctypes.byref(shape), _ptr(workspace), _ws_bytes(workspace),
                                                       _stream(stream))
     if status:

@@ -76,8 +76,14 @@ struct Struct {   // an object of that ctypes class
 };
 using Shape = Struct<pkv_attn_shape, &g_shape_type>;
 using Rope = Struct<pkv_rope_shape, &g_rope_type>;
-struct Number32 : Number {   // of those that do not fit ctypes takes the lower bits; they are left to it
-  bool take(PyObject* o) { return Number::take(o) && v == (int32_t)v; }
+struct Number32 : Number {   // those that do not fit are left to the caller
+  bool take(PyObject* o) {
+    int overflow = 0;
+    if (!PyLong_Check(o)) return false;
+    const long x = PyLong_AsLongAndOverflow(o, &overflow);
+    v = x;
+    return !overflow && x == (int32_t)x;
+  }
 };
 struct Stream {   // a handle, an object that has one, or None for the current device's current stream
   void* p = nullptr;

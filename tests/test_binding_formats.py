@@ -2,6 +2,7 @@
 which one was called and with what."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from paper_2602_11530_amd import binding as pkv
@@ -68,3 +69,28 @@ def test_each_call_reaches_its_own_entry_point(called, name):
         want.append(1 << 30)
     plain = [a.value if hasattr(a, "value") else as_c(a._obj) if hasattr(a, "_obj") else a for a in args]
     assert plain == [*want, 48]
+
+
+@pytest.mark.parametrize("module", [False, True])
+@pytest.mark.parametrize("name", [n for n in CALLS if "window" in n])
+@pytest.mark.parametrize("where", [0, 1])
+def test_numbers_of_tokens_beyond_32_bits(monkeypatch, name, module, where):
+    """Refused, not cut to their lower bits; whole numbers of another class are taken."""
+    pkv.lib()
+    if not module:
+        monkeypatch.setattr(pkv, "_call", pkv._ByCtypes())
+    args = list(CALLS[name])
+    at = 8 if "fp8" in name else 6
+    empty = pkv.make_shape(0, 8, 2, 19, 128)
+    args = [empty if a is SHAPE else a for a in args]
+    for bad in (2 ** 31, 2 ** 32 + 5, -2 ** 31 - 1, 2 ** 70, -1):
+        args[at + where] = bad
+        with pytest.raises(pkv.PkvError) as e:
+            getattr(pkv, name)(*args, 0)
+        assert e.value.status == pkv.PKV_ERR_SHAPE
+    for good in (np.int64(5), np.int32(2 ** 31 - 1), 0):
+        args[at + where] = good
+        getattr(pkv, name)(*args, 0)
+    args[at + where] = 5.0
+    with pytest.raises(TypeError):
+        getattr(pkv, name)(*args, 0)

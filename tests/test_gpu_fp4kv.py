@@ -43,6 +43,16 @@ def test_append_writes_its_rows_and_nothing_else(device, dim, block, hq, hkv):
     assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("dim,hkv", [(64, 3), (128, 8), (256, 7)])
+def test_append_for_many_requests(device, dim, hkv):
+    b = make_batch(np.random.default_rng(1).integers(0, 40, 1200), hkv, hkv, dim, 16, seed=24)
+    pools = pools_of(b, "fp4")
+    new = [wl.normal_bf16(b.rng, (len(b.lens), hkv, dim)) for _ in range(2)]
+    got = append(b, pools, *new)
+    want = expected(b, pools, *new, b.lens, [s for s, n in enumerate(b.lens) if n])
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+
+
 def test_append_of_every_kind_of_value(device):
     """Every finite bf16 value as the largest of a group, all ties between codes, values below a group's smallest, infinities and NaN."""
     rng = np.random.default_rng(5)
