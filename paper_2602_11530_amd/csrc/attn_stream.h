@@ -45,6 +45,14 @@
 //         eight 16-byte V loads (a 256-byte run per token per load), sixteen
 //         output tiles; a block is 16 KiB here and a wavefront needs more than half
 //         of a SIMD's registers, so one wavefront per SIMD streams (half as many).
+// E2M1 tiles (fp4.h): two of them, 32 tokens, at a time.  The order of bytes in a tile is that of the lanes, so a load is a row of bytes in a row and
+// nothing is turned.  Lane (n, c) has 32 dims of token n (16 at D = 64), widened with their scale to D/32 operands of S^T, two codes an
+// instruction, and tokens 4*c .. 4*c + 3 of V, so that P is an operand of 32 tokens and the second product takes v_mfma_f32_16x16x32_bf16.
+// Against a tile at a time, append and attention, us: 64 requests of 1024..8192 tokens on 40/8 heads 66.9 / 66.1, at D = 64 55.8 / 49.3, at
+// D = 256 123.2 / 116.0; 64 of 100..600 17.6 / 19.2, 8 at D = 256 19.3 / 20.5.  Scores by v_mfma_scale_f32_16x16x128_f8f6f4 would take the
+// codes as they are, but that instruction adds its 128 products with an error of up to 6e-5 of the sum of their magnitudes.
+// A span (window and sinks): the units that hold a token to be seen are the stream, in order; of a unit of which some are not seen the scores and weights
+// are replaced by select and V's rows by zeros, as those behind a request's last token are.
 // The running maximum m is only raised when a score exceeds it by more than
 // 2^kLazyLog2; any reference value gives the same softmax, and the bound keeps
 // every weight within fp32/bf16 range.
@@ -72,6 +80,8 @@
 //       out once K is there, the rest of that K after the block, at D = 128 4 to 6 KiB at any time, 8 in short shares.  With 8 KiB some dies of the
 //       chip get more than their part and the others end late (64 requests 191.9 us instead of 188.9, 128 long ones 584
 //       instead of 578; with 4 KiB 4-KiB blocks lose a quarter, which is why those have all of theirs ahead)
+//   tiles: K of the next pair but one goes out when K of this one has been widened, then V, two to four tiles at any time (1.1 KiB of K and of V each at
+//       D = 128); with three or four pairs 0 to 6 % slower, short shares most
 // Deeper rings (3 or 7 blocks ahead) only lengthen the queues.
 // Finished rows and records wait in LDS and are written in
 // bursts of full-width write-through stores that the compiler's wait-count
