@@ -5,7 +5,7 @@
 //   (a, b) -> (a cos - b sin, b cos + a sin)    pairs (j, j + R/2) or (2j, 2j + 1) of the first R dims; cos and sin from the position's row
 //
 // in fp32, rounded once to what is stored.  Prompts are bound by memory, each row in and out once (16 of 100..2000 tokens on 40/8 heads, 505 MB,
-// 88 us: 5.7 TB/s, a 1 GiB copy 4.8), a step's few tokens by the launch and three round trips: lengths, the position's row and table entry,
+// 86 us: 5.9 TB/s, a 1 GiB copy 4.8), a step's few tokens by the launch and three round trips: lengths, the position's row and table entry,
 // stores.  D / 8 lanes have a row, and a lane two pieces of four dims: with pairs (j, j + R/2) those of both
 // halves, so that a rotation stays in the lane, else (and behind the first R dims) eight in a row.  The sum of squares is all that lanes
 // exchange.
@@ -194,7 +194,10 @@ struct Lane {
         for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
 #pragma unroll
         for (int m = 1; m < kLanes; m <<= 1) sum += __shfl_xor(sum, m);
-        const float inv = __builtin_amdgcn_rsqf(sum * (1.f / kD) + a.eps);   // within a unit in the last place
+        const float mean = sum * (1.f / kD) + a.eps;
+        // within a unit in the last place; the instruction takes subnormal numbers for zero
+        const bool small = mean < 0x1p-126f;
+        const float inv = __builtin_amdgcn_rsqf(small ? mean * 0x1p48f : mean) * (small ? 0x1p24f : 1.f);
         float w[8];
         unpack(choose(is_q, q_norm, k_norm), w);
 #pragma unroll

@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 EPS = 1e-5
 
 
-def run(b, pools, starts=None, tokens=None, rotary=None, interleaved=False, norm=(True, True), gap=0, max_ctx=0, in_place=False, scale=1.0, lens=None):
+def run(b, pools, starts=None, tokens=None, rotary=None, interleaved=False, norm=(True, True), gap=0, max_ctx=0, in_place=False, scale=1.0, lens=None, eps=EPS):
     """One call on random rows: inputs and outputs as values on the host."""
     hq, hkv, dim, rng = b.hq, b.hkv, b.dim, b.rng
     T = len(b.lens) if starts is None else tokens if tokens is not None else int(starts[-1])
@@ -31,7 +31,7 @@ def run(b, pools, starts=None, tokens=None, rotary=None, interleaved=False, norm
     if in_place:
         q_d, q_stride = to_dev(q_rows), 0
     q_out = q_d if in_place else torch.full((T, hq, dim), 0x7FC1, dtype=torch.int16, device="cuda")
-    rope = pkv.make_rope(T, rotary, bound, interleaved=interleaved, norm_eps=EPS, q_stride=q_stride, k_stride=width, v_stride=width)
+    rope = pkv.make_rope(T, rotary, bound, interleaved=interleaved, norm_eps=eps, q_stride=q_stride, k_stride=width, v_stride=width)
     name = "kv_rope_append" + {"bf16": "", "fp8": "_fp8", "fp4": "_fp4"}[pools.kind]
     scales = (K_SCALE, V_SCALE) if pools.kind == "fp8" else ()
     getattr(pkv, name)(q_d, d[:, hq * dim:], d[:, (hq + hkv) * dim:], *[None if w is None else to_dev(w) for w in weights],
@@ -43,8 +43,8 @@ def run(b, pools, starts=None, tokens=None, rotary=None, interleaved=False, norm
     x = wl.bf16_bits_to_f64(rows).reshape(T, width)[:, :(hq + 2 * hkv) * dim].reshape(T, -1, dim)
     at = table[[max(p, 0) for _, p in found]]
     w = [None if v is None else wl.bf16_bits_to_f64(v).reshape(dim) for v in weights]
-    q, q_size = plain.turn(x[:, :hq], w[0], at, interleaved, EPS)
-    k, k_size = plain.turn(x[:, hq:hq + hkv], w[1], at, interleaved, EPS)
+    q, q_size = plain.turn(x[:, :hq], w[0], at, interleaved, eps)
+    k, k_size = plain.turn(x[:, hq:hq + hkv], w[1], at, interleaved, eps)
     return dict(found=found, q=q, q_size=q_size, k=k, k_size=k_size, v=x[:, hq + hkv:], q_out=to_bits(q_out).reshape(T, hq, dim), q_rows=q_rows,
                 rows=rows)
 
@@ -250,6 +250,16 @@ def test_small_and_large_rows(device, scale):
     check(b, pools, run(b, pools, scale=scale))
     pools = pools_of(b, "bf16")
     check(b, pools, run(b, pools, scale=0.0))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_mean_squares_below_the_normal_numbers(device, dim):
+    # without an epsilon: rows of about 2^-66, whose mean square of 2^-132 is a subnormal number of fp32.  Squares, their sums and the mean are each
+    # off by at most 2^-150, the mean so by less than 3 * 2^-150, which is 2^-16.4 of it, and half of that in the root
+    b = make_batch([17, 5, 64, 1], 8, 2, dim, 32, seed=60)
+    r = run(b, pools_of(b, "bf16"), scale=2.0 ** -66, eps=0.0)
+    assert np.isfinite(r["q"]).all() and np.abs(r["q"]).max() > 1
+    plain.within(r["q_out"], r["q"], 2.0 ** -8 * np.abs(r["q"]) + arithmetic(r["q_size"], dim) + 2.0 ** -16 * r["q_size"])
 
 
 def test_infinities_and_nan_stay_in_their_rows(device):
