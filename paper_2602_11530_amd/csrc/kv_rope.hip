@@ -57,13 +57,14 @@ __device__ __forceinline__ void put_bf16(char* row, int p0, int p1, const float 
 }
 // Divided by the pool's scale, clamped to the format's range and rounded to nearest even by the hardware conversion.  `inverse`: the scale's
 // rounded reciprocal, or 0.  With it a product and its remainder give the rounded quotient (Markstein's theorem) in three operations instead
-// of ten, wherever the quotient is in range.
+// of ten, wherever the quotient is in range.  The remainder is taken as product less dividend: of a zero it is +0 for either sign, and less
+// that a zero keeps its own, as a quotient does.
 __device__ __forceinline__ void put_fp8(char* row, int p0, int p1, const float (&y)[8], float scale, float inverse) {
   float z[8];
   if (inverse != 0.f) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float q = y[i] * inverse, exact = __builtin_fmaf(__builtin_fmaf(-q, scale, y[i]), inverse, q);
+      const float q = y[i] * inverse, exact = __builtin_fmaf(-__builtin_fmaf(q, scale, -y[i]), inverse, q);
       z[i] = to_range(__builtin_fabsf(q) < 512.f ? exact : q);
     }
   } else {
