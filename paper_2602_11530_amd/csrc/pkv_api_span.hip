@@ -13,16 +13,16 @@ int attend(const void* q, const void* k_pool, const void* v_pool, const int32_t*
   int rc = check_shape(shape, &g);
   if (rc != PKV_OK) return rc;
   if (!(k_scale > 0.f) || !(v_scale > 0.f) || !(k_scale < __builtin_inff()) || !(v_scale < __builtin_inff())) return PKV_ERR_SHAPE;
-  Span span = {0, 0};
+  Span given = {0, 0};
   if (window) {
     if (*window < 0 || *sinks < 0) return PKV_ERR_SHAPE;
-    span.window = *window < g.max_ctx ? *window : g.max_ctx;   // no request is longer
-    span.sinks = *sinks < g.max_ctx ? *sinks : g.max_ctx;
+    given = {*window, *sinks};
   }
+  const Span span = {given.window < g.max_ctx ? given.window : g.max_ctx, given.sinks < g.max_ctx ? given.sinks : g.max_ctx};   // no request is longer
   const Span* seen = window ? &span : nullptr;
   AttnLaunch a;
   bool empty = false;
-  rc = prepare_attn(block_tables, context_lens, scale, kv_fp8, seen, shape, workspace, workspace_bytes_given, &a, &empty);
+  rc = prepare_attn(block_tables, context_lens, scale, kv_fp8, window ? &given : nullptr, shape, workspace, workspace_bytes_given, &a, &empty);
   if (rc != PKV_OK || empty) return rc;
   rc = check_layer_pointers(q, k_pool, v_pool, out);
   if (rc != PKV_OK) return rc;

@@ -84,9 +84,10 @@ inline int launch_status(hipError_t e) {
 }
 
 // Validation shared by the single-layer and the multi-layer call; fills the
-// launch descriptor except for the per-layer pointers.  `span`: of requests that see part of their context, else nullptr.
+// launch descriptor except for the per-layer pointers.  `given`: window and sinks of requests that see part of their context, as the caller has
+// them, else nullptr.
 inline int prepare_attn(const int32_t* block_tables, const int32_t* context_lens, float scale, int kv_fp8,
-                        const Span* span, const pkv_attn_shape* shape, void* workspace, size_t workspace_bytes_given,
+                        const Span* given, const pkv_attn_shape* shape, void* workspace, size_t workspace_bytes_given,
                         AttnLaunch* a, bool* empty) {
   Geometry g;
   const int rc = check_shape(shape, &g);
@@ -111,10 +112,11 @@ inline int prepare_attn(const int32_t* block_tables, const int32_t* context_lens
   a->waves = kLayerGroups * group_waves(shape->head_dim);
   const int group = group_waves(shape->head_dim);
   const int64_t segments = (int64_t)a->S * a->Hkv;
-  const int64_t max_blocks = span ? span->most_units(g.max_ctx) : (g.max_ctx + kBlockTokens - 1) / kBlockTokens;
+  const int64_t max_blocks = given ? given->most_units(g.max_ctx) : (g.max_ctx + kBlockTokens - 1) / kBlockTokens;
   a->short_blocks = kv_fp8 == kFp4Pools ? short_segment_fp4(segments, a->D) : short_segment(segments, a->D, kv_fp8);
   a->leaves_records = 1;
-  if (cut_by_segment(segments, a->D, span, kv_fp8 == kFp4Pools) && max_blocks <= a->short_blocks) {
+  const bool bounded = given && given->most_units() <= a->short_blocks;
+  if (cut_by_segment(segments, a->D, bounded, kv_fp8 == kFp4Pools) && max_blocks <= a->short_blocks) {
     // Cut along its segments, a workgroup for each.  Nothing is left in the workspace, and the layers of such
     // a launch may be more than it has room for.
     a->leaves_records = 0;

@@ -99,14 +99,17 @@ inline int short_segment_fp4(int64_t segments, int D) {
   return segments <= 64 ? short_segment(segments, D, true) : 12 * group_waves(D);
 }
 
-// Is a batch of segments that are short enough cut along them?  Where each has a workgroup that starts at once: one on a compute unit, or two at
-// D = 64 with a span or tiles, whose registers and LDS leave room for that.  With a span, where segments are alike, also in two turns if the
-// second is half full or more.  Us by records / cut, 64 requests on 40/8 heads (512 segments): window of 64 at D = 64 11.0 / 7.6, e4m3 11.7 / 7.7,
-// of 300 14.8 / 11.8, e4m3 13.6 / 9.2, tiles 13.2 / 9.9, tiles of 300..768 tokens 18.9 / 15.5; in two turns window of 64 at D = 128 13.4 / 11.5,
-// of 300 22.3 / 20.9, e4m3 16.0 / 15.5, at D = 256 37.8 / 35.6; with 48 requests 18.6 / 18.3, with 36 16.3 / 17.1, in three turns with 72 24.1 / 26.8.
-inline bool cut_by_segment(int64_t segments, int D, bool span, bool tiles) {
-  if (D == 64 && (span || tiles)) return segments <= 2 * kLayerGroups;
-  return segments <= kLayerGroups || (span && !tiles && 2 * segments >= 3 * kLayerGroups && segments <= 2 * kLayerGroups);
+// Is a batch of segments that are short enough by the bounds cut along them?  Up to kLayerGroups of them: where the bound on the lengths does not
+// say that they are short, the general launch finds it out and cuts them in the same places.  Beyond, that launch has no workgroups for them, so only
+// where the window and the sinks alone keep every segment short (`bounded`): a rule that took the bound on the lengths would let the rows' last bits
+// go by it.  At D = 64 two workgroups start at once on a compute unit, registers and LDS leave room for that; else in two turns, if the second is half
+// full or more, not with tiles.  Us by records / cut, 64 requests on 40/8 heads (512 segments): window of 64 at D = 64 11.0 / 7.6, e4m3 11.7 / 7.7, of
+// 300 14.8 / 11.8, e4m3 13.6 / 9.2, tiles 13.2 / 9.9; in two turns window of 64 at D = 128 13.4 / 11.5, of 300 22.3 / 20.9, e4m3 16.0 / 15.5,
+// at D = 256 37.8 / 35.6; with 48 requests 18.6 / 18.3, with 36 16.3 / 17.1, in three turns with 72 24.1 / 26.8.  What by the bound on the lengths
+// alone is short goes by records: tiles of 300..768 tokens at D = 64 18.9 us, cut 15.5.
+inline bool cut_by_segment(int64_t segments, int D, bool bounded, bool tiles) {
+  if (segments <= kLayerGroups) return true;
+  return bounded && segments <= 2 * kLayerGroups && (D == 64 || (!tiles && 2 * segments >= 3 * kLayerGroups));
 }
 
 // A segment that several workgroups share, as those of them leave it in which no later one begins: the one that it begins in and
@@ -210,9 +213,10 @@ struct Span {
     return n > 0 ? n : 0;
   }
   __host__ __device__ int units(int L) const { return units_of(L) - left_out(L); }
-  // of a request of at most `tokens`
+  // of a request of any length, and of one of at most `tokens`
+  int64_t most_units() const { return (int64_t)sink_units() + (window > 0 ? units_of(window) + 1 : 0); }
   int64_t most_units(int tokens) const {
-    const int64_t all = units_of(tokens), some = (int64_t)sink_units() + (window > 0 ? units_of(window) + 1 : 0);
+    const int64_t all = units_of(tokens), some = most_units();
     return all < some ? all : some;
   }
   // the request's unit that is the b-th of those
