@@ -1131,7 +1131,8 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   store_staged();
   // Never: up to here the registers of the loads that went out last, behind the share's end, are their own.  As far as the compiler knows
   // they may still be on their way, and a loop of stores that took one over would wait for them in every turn, and so for the
-  // acknowledgement of each hidden store.
+  // acknowledgement of each hidden store.  Of tiles two pairs are on their way; at D = 256 nothing takes the second one's registers over as it
+  // is, and keeping them too moves others about in the stream's loop (64 requests of 1024..8192 tokens 114 -> 117.5 us).
   int never = 0;
   if (!kWhole) asm volatile("s_mov_b32 %0, 0" : "=s"(never));
   if (never) {
@@ -1141,6 +1142,10 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     for (int jj = 0; jj < kKLoads; ++jj) arrived(kbuf[0][jj]);
 #pragma unroll
     for (int e = 0; e < kVLoads; ++e) arrived(vbuf[kLate][e]);
+    if constexpr (kFp4 && kD != 256) {
+      arrived_k(kbuf[1]);
+      arrived_v(vbuf[1]);
+    }
   }
   // Refused ids are reported once per wavefront, after the stream: nothing in the loop waits on it.
   if (a.id_faults && refused && lane == 0) atomicAdd(a.id_faults, refused);
