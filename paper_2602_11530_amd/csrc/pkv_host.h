@@ -113,7 +113,7 @@ inline int prepare_attn(const int32_t* block_tables, const int32_t* context_lens
   const int group = group_waves(shape->head_dim);
   const int64_t segments = (int64_t)a->S * a->Hkv;
   const int64_t max_blocks = given ? given->most_units(g.max_ctx) : (g.max_ctx + kBlockTokens - 1) / kBlockTokens;
-  a->short_blocks = kv_fp8 == kFp4Pools ? short_segment_fp4(segments, a->D) : short_segment(segments, a->D, kv_fp8);
+  a->short_blocks = kv_fp8 == kFp4Pools ? short_segment_fp4(a->D) : short_segment(segments, a->D, kv_fp8);
   a->leaves_records = 1;
   const bool bounded = given && given->most_units() <= a->short_blocks;
   if (cut_by_segment(segments, a->D, bounded, kv_fp8 == kFp4Pools) && max_blocks <= a->short_blocks) {

@@ -91,13 +91,13 @@ inline int short_segment(int64_t segments, int D, bool kv_fp8) {
   return (segments <= 64 && block_bytes >= 8192 ? 3 : 6) * group_waves(D);
 }
 
-// The same for tiles, a little more than half of what e4m3 takes.  Up to 12 blocks per wavefront where most compute units have a segment, else as
-// above.  Us for append and attention at 3 or 6 blocks, 12, 24: 256 segments of 800..1536 tokens 21.2 / 18.0 / 17.5, at D = 64 18.0 / 14.6,
-// at D = 256 of 400..768 23.3 / 18.7; 128 of 800..1536 17.5 / 16.4 / 16.5, of 1500..3000 20.9 / 21.1 / 23.9; 256 of those 25.7 / 26.1 / 25.5;
-// 8 segments of 900..1536 13.8 / 15.3, at D = 64 13.6 / 13.2.
-inline int short_segment_fp4(int64_t segments, int D) {
-  return segments <= 64 ? short_segment(segments, D, true) : 12 * group_waves(D);
-}
+// The same for tiles, a little more than half of what e4m3 takes: up to 12 blocks per wavefront.  Us for append and attention at 3 or 6 blocks, 12, 24:
+// 256 segments of 800..1536 tokens 21.2 / 18.0 / 17.5, at D = 64 18.0 / 14.6, at D = 256 of 400..768 23.3 / 18.7; 128 of 800..1536 17.5 / 16.4 / 16.5,
+// of 1500..3000 20.9 / 21.1 / 23.9; 256 of those 25.7 / 26.1 / 25.5.  Few segments, by replays of a graph, at 3, 6, 12: 8 of 900..1150 12.3 / 12.3 /
+// 11.6, at D = 64 11.8 / 11.8 / 10.5, at D = 256 of 300..384 13.5 / 11.6 / 11.6; 64 of 900..1150 14.4 / 14.4 / 13.8, at D = 64 13.5 / 13.5 / 12.0, at
+// D = 256 of 300..384 16.3 / 11.8 / 11.8, of 600..768 16.9 / 16.9 / 15.4.  12 loses where up to 8 segments reach it: 8 of 1200..1536 13.2 / 13.2 / 13.9,
+// at D = 256 of 600..768 14.5 / 14.5 / 15.1.
+inline int short_segment_fp4(int D) { return 12 * group_waves(D); }
 
 // Is a batch of segments that are short enough by the bounds cut along them?  Up to kLayerGroups of them: where the bound on the lengths does not
 // say that they are short, the general launch finds it out and cuts them in the same places.  Beyond, that launch has no workgroups for them, so only

@@ -26,3 +26,21 @@ def test_rows_are_the_same_under_every_bound(device, dim, kind, window, sinks, s
     plain.within(loose[some], want, off)
     for bound in (int(b.lens.max()), 700, 1000):
         assert np.array_equal(attend(b, pools, window, sinks, max_context_len=bound), loose), bound
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("window,sinks", [(None, None), (500, 70), (5000, 0)])
+@pytest.mark.parametrize("seqs,hkv", [(1, 1), (1, 8), (8, 8), (9, 8)])
+def test_few_segments_of_tiles_up_to_the_longest_that_are_cut(device, dim, window, sinks, seqs, hkv):
+    """Segments of up to 12 units a wavefront, a token less and a unit more."""
+    longest = 16 * 12 * (4 if dim == 256 else 8)
+    for most in (longest, longest - 17, longest + 1):
+        b = make_batch([most, *np.random.default_rng(3).integers(1, most, seqs - 1)], 2 * hkv, hkv, dim, 16, seed=seqs + most)
+        wide = np.full((seqs, 2 * longest // 16), -1, np.int32)
+        wide[:, :b.tables.shape[1]] = b.tables
+        b.tables = wide
+        pools = pools_of(b, "fp4")
+        loose = attend(b, pools, window, sinks)
+        want, off = plain.attention(b.q, pools.k, pools.v, b.tables, b.lens, b.scale, window, sinks or 0)
+        plain.within(loose, want, off)
+        assert np.array_equal(attend(b, pools, window, sinks, max_context_len=most), loose)
