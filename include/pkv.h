@@ -68,7 +68,9 @@ typedef struct {
                                  longer by the bound than 384 to 768 tokens (192 to 384 at
                                  D = 256), attention is one launch instead of two, and
                                  append and attention take 0.70 to 0.78 of the time
-                                 (requests of 10..300 tokens).                           */
+                                 (requests of 10..300 tokens).  Over 4-bit pools up to
+                                 1536 tokens (768 at D = 256); with a window what counts
+                                 is what a request sees.                                 */
   int64_t num_pool_blocks;    /* NB: physical blocks in k_pool and in v_pool;
                                  1 <= NB and NB * Hkv * B/16 < 2^31                      */
 } pkv_attn_shape;
@@ -186,7 +188,7 @@ int paged_decode_attn_fp8kv(const void* q, const void* k_pool, const void* v_poo
                             void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * Pools held in 4 bits, a quarter of the bytes of bf16: values of OCP FP4 E2M1 (a
+ * Pools held in 4 bits, 17/64 of the bytes of bf16: values of OCP FP4 E2M1 (a
  * sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
  * negatives), and for each group of 32 dims of a token and KV head one scale byte
  * b that stands for 2^(b - 127) (OCP E8M0; 255 is NaN).  A pool is an array of

@@ -22,7 +22,8 @@
 //   cut along them   one workgroup per segment, which meets in LDS and finishes it: no records, and no
 //                    reduce pass where the bounds say so beforehand (4 requests of 17..300 tokens on 8/2
 //                    heads: 14.0 -> 11.3 us and a launch less on the host).  Few and short ones, up to 3
-//                    or 6 blocks per wavefront (short_segment).
+//                    or 6 blocks per wavefront (short_segment), of tiles 12 (short_segment_fp4), and with a window and sinks that
+//                    keep all short up to twice as many (cut_by_segment).
 //
 // Per 16-token block, lane = 16*c + n, head_dim D = 128 (64 and 256 below):
 //   S^T = K . Q^T   D/32 v_mfma_f32_16x16x32_bf16 (k = 32 dims each).
@@ -617,7 +618,9 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   // The loads of a block, nontemporal: the stream is read once and must not allocate in the
   // caches it passes through.  The loads are unconditional so that every wait in the loop knows
   // exactly how many are outstanding, and their bounds are the block's valid rows: what lies behind a
-  // request's last token, a block that is unmapped and an index past the share's end are not read and arrive as zeros.
+  // request's last token, a block that is unmapped and an index past the share's end are not read and arrive as zeros.  A tile's rows lie
+  // across it, so one with a valid token is read whole: what the other tokens' bytes give never counts, their scores and weights are replaced
+  // and V's scales cleared (attend_pair).
   // Against whole blocks, the first one of the pool past a share's end, and descriptors looked up for each load: 512 requests of
   // 16..512 tokens 109.5 -> 106.0 us, shares of 1 to 4 blocks at D = 128 0.98 of the time, 72 shapes of 8-bit pools at D = 64 0.983.
   auto rows_of = [&](const void* pool, Block at) {

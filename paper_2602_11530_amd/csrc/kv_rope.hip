@@ -7,8 +7,9 @@
 // in fp32, rounded once to what is stored.  Prompts are bound by memory, each row in and out once (16 of 100..2000 tokens on 40/8 heads, 505 MB,
 // 86 us: 5.9 TB/s, a 1 GiB copy 4.8), a step's few tokens by the launch and three round trips: lengths, the position's row and table entry,
 // stores.  D / 8 lanes have a row, and a lane two pieces of four dims: with pairs (j, j + R/2) those of both
-// halves, so that a rotation stays in the lane, else (and behind the first R dims) eight in a row.  The sum of squares is all that lanes
-// exchange.
+// halves, so that a rotation stays in the lane, else (and behind the first R dims) eight in a row.  Into bf16 and e4m3 pools the sum of squares is all
+// that lanes exchange; tiles want a key's dims eight in a row, which are taken from the lanes that have them, and the largest of a group of 32, which is
+// four lanes' (the prompts above 89 us, 453 MB).
 #include "fp4.h"
 #include "pkv_kernels.h"
 
@@ -352,6 +353,9 @@ void launch_passes(const RopeLaunch& a, hipStream_t stream) {
 // Few tokens: as many workgroups as their rows give.  Many: up to four rows a lane, for which a position is looked up once; where a token's rows
 // do not fill a workgroup, rows of several tokens.  Us for 16 prompts of 100..2000 tokens: 40/8 heads 88, the rows in a row 111, at D = 256 176 /
 // 208, 28/4 heads 66 / 72; 8/2 heads 27.8 / 23.7, 8/1 26.8 / 21.0, at D = 64 23.2 / 12.1, 16/8 there 30.5 / 28.6.
+// Where many begins: us of the two ways for a step of 256, 512, 1000, 2000 requests, by replays of a graph (few / many): 40/8 heads 3.6 / 4.5, 4.7 / 5.1,
+// 7.6 / 7.4, 12.8 / 11.0, tiles 4.0 / 4.6, 5.5 / 5.7, 8.3 / 8.4, 14.1 / 12.3; 32/8 at D = 64 3.1 / 3.5, 3.7 / 3.7, 4.7 / 4.5, 8.0 / 6.6; 16/8 at D = 256
+// 3.6 / 4.6, 4.8 / 5.2, 7.8 / 7.9, 13.1 / 12.2; 8/1 2.9 / 4.0, 3.1 / 4.1, 3.6 / 4.3, 4.7 / 4.8.
 template <int kD>
 void launch_dim(const RopeLaunch& a, hipStream_t stream) {
   const int rows = a.Hq + 2 * a.Hkv, at_a_time = kThreads / (kD / 8);

@@ -200,7 +200,7 @@ struct AttnLayers {
 struct OneLayer {};
 struct GroupPerSegment {};   // a workgroup for each segment
 struct WholeLayer : OneLayer, GroupPerSegment {};
-// Which tokens a request of L sees: its last `window`, and its first `sinks`.  Both are at most the longest context.  Of its 16-token units
+// Which tokens a request of L sees: its last `window`, and its first `sinks`.  On the device both are at most the longest context.  Of its 16-token units
 // those that hold such a token are attended over, in order; what lies between the sinks and the window is no part of the stream.
 struct Span {
   int window, sinks;
