@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("kind,window,sinks", [(k, w, s) for k in KINDS for w, s in ((60, 4), (150, 20), (2000, 4))]
                          + [("fp4", None, None)])
-@pytest.mark.parametrize("seqs,hkv", [(32, 8), (50, 6), (96, 4), (128, 4)])
+@pytest.mark.parametrize("seqs,hkv", [(32, 8), (60, 5), (96, 4), (128, 4)])
 def test_rows_are_the_same_under_every_bound(device, dim, kind, window, sinks, seqs, hkv):
     rng = np.random.default_rng(seqs + dim)
     b = make_batch(rng.integers(0, 200, seqs), 2 * hkv, hkv, dim, 16, seed=seqs)
@@ -36,7 +36,7 @@ def test_few_segments_of_tiles_up_to_the_longest_that_are_cut(device, dim, windo
     longest = 16 * 12 * (4 if dim == 256 else 8)
     for most in (longest, longest - 17, longest + 1):
         b = make_batch([most, *np.random.default_rng(3).integers(1, most, seqs - 1)], 2 * hkv, hkv, dim, 16, seed=seqs + most)
-        wide = np.full((seqs, 2 * longest // 16), -1, np.int32)
+        wide = np.full((seqs, 5 * longest // 32), -1, np.int32)
         wide[:, :b.tables.shape[1]] = b.tables
         b.tables = wide
         pools = pools_of(b, "fp4")

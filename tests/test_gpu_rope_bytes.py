@@ -17,7 +17,7 @@ SCALES = {"bf16": [()], "fp4": [()],     # beyond 2^60 the quotient is divided o
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_rows_as_they_are_are_the_append(device, kind, scales, dim):
     """Every bf16 value, zeros of both signs, infinities and NaN among them: without norm and rotation the bytes are the append's."""
-    S, hkv = 65536 // (4 * dim), 4
+    S, hkv = 65536 // (2 * dim), 2
     bits = np.arange(65536, dtype=np.uint16).reshape(S, hkv, dim)
     b = make_batch(np.full(S, 5), 1, 1, dim, 16, seed=70)
     b.hq = b.hkv = hkv
