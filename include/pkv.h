@@ -226,6 +226,39 @@ int paged_decode_attn_fp4kv(const void* q, const void* k_pool, const void* v_poo
                             size_t workspace_bytes, void* stream);
 
 /*
+ * Pools held in 8 bits with a scale for each block and KV head.  A pool is e4m3
+ * bytes [NB][Hkv][B][D] as in paged_decode_attn_fp8kv, and with it goes an array of
+ * bytes [NB][row], row = Hkv rounded up to a multiple of 16 (pkv_fp8blk_scale_bytes):
+ * byte b of block id and KV head kvh stands for 2^(b - 127) (OCP E8M0; 255 is NaN),
+ *
+ *     K[.] = 2^(k_scales[id][kvh] - 127) * e4m3(k_pool byte),     V alike.
+ *
+ * One scale per pool has to be found beforehand and covers the head and the token
+ * with the largest values; these are found by the appends, block by block.  The
+ * copies (gather, scatter, move, offload, reload) take the pool as they take one of
+ * paged_decode_attn_fp8kv, and its scales as a pool of blocks of `row` bytes.  The
+ * paper fixes no quantised format: this one is the library's choice.
+ */
+int pkv_fp8blk_scale_bytes(const pkv_attn_shape* shape /* host */, size_t* out_bytes);
+
+/*
+ * paged_decode_attn over such pools (q and out bf16, fp32 arithmetic).  Byte and scale
+ * are widened together to bf16, exactly for scale bytes of 10 to 246, the ones that the
+ * appends write, so the result is the attention of the de-quantised pools to the same
+ * tolerance as the bf16 call.  Scales of blocks that hold no token of a request are not
+ * used; unused slots and unused blocks may hold any bytes.
+ *
+ *   k_pool, v_pool      device  e4m3  [NB][Hkv][B][D]
+ *   k_scales, v_scales  device  uint8 [NB][row]; out must not overlap them (PKV_ERR_SHAPE)
+ *   shape               as for paged_decode_attn: every head_dim and block_size
+ */
+int paged_decode_attn_fp8blk(const void* q, const void* k_pool, const void* v_pool,
+                             const uint8_t* k_scales, const uint8_t* v_scales,
+                             const int32_t* block_tables, const int32_t* context_lens, float scale,
+                             void* out, const pkv_attn_shape* shape, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
  * Decode attention of requests that see part of their context: the last `window`
  * tokens (the one being decoded is one of them) and the first `sinks` ones:
  *
@@ -410,6 +443,27 @@ int kv_append_fp4(const void* k_new, const void* v_new, void* k_pool, void* v_po
                   const int32_t* block_tables, const int32_t* context_lens,
                   const pkv_attn_shape* shape, void* stream);
 
+/*
+ * kv_append for pools with a scale for each block and KV head.  Let e be the least
+ * power, from -117 to 119, with which no finite value that the call writes into a block
+ * for a KV head is beyond 448 * 2^e.
+ *   A block whose first slot the call writes takes the scale 2^e, whatever it held.
+ *   Any other block keeps its scale if that is 2^e or more.  If not it takes 2^e, and
+ *   the rows in the slots before the first one that the call writes are rounded to it:
+ *   byte = e4m3(e4m3(byte) * old / new).
+ * New values are stored as byte = e4m3(x / scale), round to nearest even, zeros keeping
+ * their sign, magnitudes beyond 448 * scale (infinity, or above 448 * 2^119) held there,
+ * NaN as NaN.  K and V have their own scales.  Of a block that other requests have in
+ * their tables no token may be appended to (unchecked), as for every append.
+ * Everything else as for kv_append.
+ *
+ *   k_pool, v_pool      device  e4m3  [NB][Hkv][B][D]
+ *   k_scales, v_scales  device  uint8 [NB][row]
+ */
+int kv_append_fp8blk(const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                     uint8_t* k_scales, uint8_t* v_scales, const int32_t* block_tables,
+                     const int32_t* context_lens, const pkv_attn_shape* shape, void* stream);
+
 /* The new tokens of one kv_rope_append call and how their rows are turned. */
 typedef struct {
   int64_t num_tokens;    /* T: rows of q, k, v and q_out, 0..2^24-1                             */
@@ -469,6 +523,65 @@ int kv_rope_append_fp4(const void* q, const void* k, const void* v, const void* 
                        void* v_pool, const int32_t* block_tables, const int32_t* context_lens,
                        const int32_t* token_starts, const pkv_rope_shape* rope /* host */,
                        const pkv_attn_shape* shape, void* stream);
+
+/*
+ * The same into pools with a scale for each block and KV head, which are chosen as in
+ * kv_append_fp8blk from the normalised and rotated rows that the call writes.  q and
+ * q_out may both be NULL: no queries.  A refused table entry counts one for each request
+ * and block that new tokens fall into.
+ */
+int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const void* q_norm,
+                          const void* k_norm, const float* cos_sin, void* q_out, void* k_pool,
+                          void* v_pool, uint8_t* k_scales, uint8_t* v_scales,
+                          const int32_t* block_tables, const int32_t* context_lens,
+                          const int32_t* token_starts, const pkv_rope_shape* rope /* host */,
+                          const pkv_attn_shape* shape, void* stream);
+
+/*
+ * Causal attention of new tokens, whole prompts or pieces of them, over the cache that
+ * kv_rope_append has just put them into: each sees the tokens of its request up to itself,
+ *
+ *   out[i,h,:] = sum_t softmax_t( scale * q[i,h,:] . K[s,t,kvh,:] ) * V[s,t,kvh,:]
+ *   for t in [0, p_i],   p_i = context_lens[s] - n_s + (i - token_starts[s]),
+ *
+ * with s, n_s and K[s,t], V[s,t] as in kv_rope_append and paged_decode_attn, over bf16
+ * pools, over e4m3 pools with a scale each (_fp8kv) and with one for each block and KV
+ * head (_fp8blk).  Rows of tokens without a position (see kv_rope_append; padding among
+ * them) are left as they were.  Tokens of blocks whose id lies outside [0, num_pool_blocks)
+ * are left out of the softmax; a row that sees no other is all zeros.  What is not finite in K or V of a token reaches the
+ * rows that see it alone, as in paged_decode_attn.  Table entries and slots behind a
+ * request's last token are never read.
+ *
+ * bf16 inputs, fp32 scores, softmax statistics and accumulation; a weight is rounded to bf16
+ * before it multiplies V (relative error 2^-8), and a row once, to bf16, at the end.  No bit of a row depends on where
+ * its blocks are nor on the other requests' contents, but its last bits depend on T, num_seqs and
+ * max_context_len, which choose how contexts are cut, and on token_starts[s] modulo the tokens of a workgroup's rows.
+ *
+ *   q             device  bf16  [T][Hq][D], rows of tokens without gaps
+ *   token_starts  device  int32 [num_seqs + 1], ascending, or NULL: one token for each request, T = num_seqs
+ *   num_tokens    T, 0..2^24-1
+ *   out           device  bf16  [T][Hq][D]; may be q itself, and must not overlap q otherwise, nor the
+ *                 pools, scales or tables (PKV_ERR_SHAPE)
+ *   shape         host    (partition_size is not used)
+ *   workspace     device, >= pkv_prompt_workspace_bytes(), 16-byte aligned; may be NULL when that is 0
+ */
+int pkv_prompt_workspace_bytes(const pkv_attn_shape* shape /* host */, int64_t num_tokens, size_t* out_bytes);
+int paged_prompt_attn(const void* q, const void* k_pool, const void* v_pool,
+                      const int32_t* block_tables, const int32_t* context_lens,
+                      const int32_t* token_starts, int64_t num_tokens, float scale, void* out,
+                      const pkv_attn_shape* shape, void* workspace, size_t workspace_bytes,
+                      void* stream);
+int paged_prompt_attn_fp8kv(const void* q, const void* k_pool, const void* v_pool,
+                            const int32_t* block_tables, const int32_t* context_lens,
+                            const int32_t* token_starts, int64_t num_tokens, float scale,
+                            float k_scale, float v_scale, void* out, const pkv_attn_shape* shape,
+                            void* workspace, size_t workspace_bytes, void* stream);
+int paged_prompt_attn_fp8blk(const void* q, const void* k_pool, const void* v_pool,
+                             const uint8_t* k_scales, const uint8_t* v_scales,
+                             const int32_t* block_tables, const int32_t* context_lens,
+                             const int32_t* token_starts, int64_t num_tokens, float scale,
+                             void* out, const pkv_attn_shape* shape, void* workspace,
+                             size_t workspace_bytes, void* stream);
 
 /*
  * Optional report of block ids the kernels refused to follow.  No kernel of this

@@ -34,6 +34,8 @@ EXPORTS = (
     "pkv_fp4_block_bytes", "kv_append_fp4", "paged_decode_attn_fp4kv", "paged_decode_attn_window",
     "paged_decode_attn_window_fp8kv", "paged_decode_attn_window_fp4kv", "kv_rope_append", "kv_rope_append_fp8",
     "kv_rope_append_fp4",
+    "pkv_fp8blk_scale_bytes", "paged_decode_attn_fp8blk", "kv_append_fp8blk", "kv_rope_append_fp8blk",
+    "pkv_prompt_workspace_bytes", "paged_prompt_attn", "paged_prompt_attn_fp8kv", "paged_prompt_attn_fp8blk",
 )
 
 
@@ -170,7 +172,15 @@ def lib() -> ctypes.CDLL:
                 ("paged_decode_attn_window_fp4kv", attn + [i32, i32, vp, shp, vp, size, vp]),
                 ("kv_rope_append", rows + [rope, shp, vp]),
                 ("kv_rope_append_fp8", rows + [f32, f32, rope, shp, vp]),
-                ("kv_rope_append_fp4", rows + [rope, shp, vp])):
+                ("kv_rope_append_fp4", rows + [rope, shp, vp]),
+                ("pkv_fp8blk_scale_bytes", [shp, ctypes.POINTER(size)]),
+                ("paged_decode_attn_fp8blk", [vp] * 5 + [i32p, i32p, f32, vp, shp, vp, size, vp]),
+                ("kv_append_fp8blk", [vp] * 6 + [i32p, i32p, shp, vp]),
+                ("kv_rope_append_fp8blk", [vp] * 11 + [i32p] * 3 + [rope, shp, vp]),
+                ("pkv_prompt_workspace_bytes", [shp, i64, ctypes.POINTER(size)]),
+                ("paged_prompt_attn", [vp] * 3 + [i32p] * 3 + [i64, f32, vp, shp, vp, size, vp]),
+                ("paged_prompt_attn_fp8kv", [vp] * 3 + [i32p] * 3 + [i64, f32, f32, f32, vp, shp, vp, size, vp]),
+                ("paged_prompt_attn_fp8blk", [vp] * 5 + [i32p] * 3 + [i64, f32, vp, shp, vp, size, vp])):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = ctypes.c_int
         _raw_stream = _find_raw_stream(torch)
@@ -249,6 +259,20 @@ def pkv_fp4_block_bytes(shape: AttnShape) -> int:
     return int(n.value)
 
 
+def pkv_fp8blk_scale_bytes(shape: AttnShape) -> int:
+    """Bytes of a block's scales in a pool with a scale for each block and KV head: a row of the array, and the size of its images in the copies."""
+    n = ctypes.c_size_t(0)
+    _check(lib().pkv_fp8blk_scale_bytes(ctypes.byref(shape), ctypes.byref(n)))
+    return int(n.value)
+
+
+def pkv_prompt_workspace_bytes(shape: AttnShape, num_tokens: int) -> int:
+    """Bytes of workspace that attention of ``num_tokens`` new tokens needs, 0 as a rule where they are many."""
+    n = ctypes.c_size_t(0)
+    _check(lib().pkv_prompt_workspace_bytes(ctypes.byref(shape), _int64(num_tokens), ctypes.byref(n)))
+    return int(n.value)
+
+
 def make_rope(num_tokens, rotary_dim, num_positions, interleaved=False, norm_eps=1e-6, q_stride=0, k_stride=0,
               v_stride=0) -> RopeShape:
     """``num_positions``: rows of the table of cosines and sines; strides are in elements, 0 for rows without gaps."""
@@ -292,6 +316,13 @@ def _int32(x) -> int:
     return x
 
 
+def _int64(x) -> int:
+    x = operator.index(x)
+    if not -2 ** 63 <= x < 2 ** 63:
+        _check(PKV_ERR_SHAPE)
+    return x
+
+
 def _ws_bytes(workspace) -> int:
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
@@ -305,6 +336,19 @@ def paged_decode_attn_fp4kv(q, k_pool, v_pool, block_tables, context_lens, scale
         status = lib().paged_decode_attn_fp4kv(_ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(block_tables), _ptr(context_lens),
                                                ctypes.c_float(scale), _ptr(out), ctypes.byref(shape), _ptr(workspace),
                                                _ws_bytes(workspace), _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_decode_attn_fp8blk(q, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, scale, out, shape: AttnShape,
+                             workspace=None, stream=None) -> None:
+    """Attention over e4m3 pools with a scale for each block and KV head (``pkv_fp8blk_scale_bytes`` says how long a row of scales is)."""
+    status = (_call or _native()).paged_decode_attn_fp8blk(q, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, scale, out,
+                                                           shape, workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_decode_attn_fp8blk(*map(_ptr, (q, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens)),
+                                                ctypes.c_float(scale), _ptr(out), ctypes.byref(shape), _ptr(workspace),
+                                                _ws_bytes(workspace), _stream(stream))
     if status:
         _check(status)
 
@@ -513,5 +557,67 @@ def kv_rope_append_fp4(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, 
     if status is NotImplemented:
         status = lib().kv_rope_append_fp4(*map(_ptr, (q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens,
                                                       token_starts)), ctypes.byref(rope), ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def kv_append_fp8blk(k_new, v_new, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, shape: AttnShape, stream=None) -> None:
+    """Quantise each request's newest K and V rows with their block's scales, which grow as they have to, and write them into slot
+    context_lens[s] - 1."""
+    status = (_call or _native()).kv_append_fp8blk(k_new, v_new, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, shape, stream)
+    if status is NotImplemented:
+        status = lib().kv_append_fp8blk(*map(_ptr, (k_new, v_new, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens)),
+                                        ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def kv_rope_append_fp8blk(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, token_starts,
+                          rope: RopeShape, shape: AttnShape, stream=None) -> None:
+    """``kv_rope_append`` into e4m3 pools with a scale for each block and KV head; ``q`` and ``q_out`` may both be None."""
+    status = (_call or _native()).kv_rope_append_fp8blk(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, k_scales, v_scales, block_tables,
+                                                        context_lens, token_starts, rope, shape, stream)
+    if status is NotImplemented:
+        status = lib().kv_rope_append_fp8blk(*map(_ptr, (q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, k_scales, v_scales, block_tables,
+                                                         context_lens, token_starts)), ctypes.byref(rope), ctypes.byref(shape), _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_prompt_attn(q, k_pool, v_pool, block_tables, context_lens, token_starts, num_tokens: int, scale, out, shape: AttnShape,
+                      workspace=None, stream=None) -> None:
+    """Causal attention of ``num_tokens`` new tokens, packed request behind request, over the cache that already holds them."""
+    status = (_call or _native()).paged_prompt_attn(q, k_pool, v_pool, block_tables, context_lens, token_starts, num_tokens, scale, out, shape,
+                                                    workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_prompt_attn(*map(_ptr, (q, k_pool, v_pool, block_tables, context_lens, token_starts)), _int64(num_tokens),
+                                         ctypes.c_float(scale), _ptr(out), ctypes.byref(shape), _ptr(workspace), _ws_bytes(workspace),
+                                         _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_prompt_attn_fp8kv(q, k_pool, v_pool, block_tables, context_lens, token_starts, num_tokens: int, scale, k_scale, v_scale, out,
+                            shape: AttnShape, workspace=None, stream=None) -> None:
+    """The same over e4m3 pools with a scale each."""
+    status = (_call or _native()).paged_prompt_attn_fp8kv(q, k_pool, v_pool, block_tables, context_lens, token_starts, num_tokens, scale, k_scale,
+                                                          v_scale, out, shape, workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_prompt_attn_fp8kv(*map(_ptr, (q, k_pool, v_pool, block_tables, context_lens, token_starts)), _int64(num_tokens),
+                                               ctypes.c_float(scale), ctypes.c_float(k_scale), ctypes.c_float(v_scale), _ptr(out),
+                                               ctypes.byref(shape), _ptr(workspace), _ws_bytes(workspace), _stream(stream))
+    if status:
+        _check(status)
+
+
+def paged_prompt_attn_fp8blk(q, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, token_starts, num_tokens: int, scale, out,
+                             shape: AttnShape, workspace=None, stream=None) -> None:
+    """The same over e4m3 pools with a scale for each block and KV head."""
+    status = (_call or _native()).paged_prompt_attn_fp8blk(q, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, token_starts,
+                                                           num_tokens, scale, out, shape, workspace, stream)
+    if status is NotImplemented:
+        status = lib().paged_prompt_attn_fp8blk(*map(_ptr, (q, k_pool, v_pool, k_scales, v_scales, block_tables, context_lens, token_starts)),
+                                                _int64(num_tokens), ctypes.c_float(scale), _ptr(out), ctypes.byref(shape), _ptr(workspace),
+                                                _ws_bytes(workspace), _stream(stream))
     if status:
         _check(status)

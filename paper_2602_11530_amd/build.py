@@ -12,8 +12,9 @@ from typing import Optional
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpkv.so")
-SOURCES = ["pkv_api.hip", "pkv_api_span.hip", "pkv_api_rope.hip", "attn_stream.hip", "attn_stream_large.hip", "attn_stream_short.hip",
-           "attn_stream_span.hip", "attn_stream_span_short.hip", "attn_stream_fp4.hip", "attn_reduce.hip", "kv_copy.hip", "kv_append.hip", "kv_rope.hip",
+SOURCES = ["pkv_api.hip", "pkv_api_span.hip", "pkv_api_rope.hip", "pkv_api_prompt.hip", "attn_stream.hip", "attn_stream_large.hip", "attn_stream_short.hip",
+           "attn_stream_span.hip", "attn_stream_span_short.hip", "attn_stream_fp4.hip", "attn_stream_blk.hip", "attn_reduce.hip", "prompt_attn.hip",
+           "kv_copy.hip", "kv_append.hip", "kv_rope.hip", "kv_append_blk.hip",
            "stream_probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

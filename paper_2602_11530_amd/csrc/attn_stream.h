@@ -165,9 +165,10 @@ __device__ __forceinline__ float bf16_round(float x, uint32_t& bits) {
 // Four e4m3 bytes of one dword -> four bf16 (exact: every e4m3 value is a bf16 value), an instruction for two of them.  By way of
 // fp32 it took two: 72 shapes at D = 64 0.983 of the time, 18 of 8 to 70 blocks a wavefront at D = 128 0.996, 64 requests of
 // 1024..8192 tokens 102.2 -> 101.5 us.
-__device__ __forceinline__ u32x2 widen_e4m3x4(uint32_t w) {
-  return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, false)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true))};
+// Times a power of two, which is exact too.
+__device__ __forceinline__ u32x2 widen_e4m3x4(uint32_t w, float scale = 1.f) {
+  return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, true))};
 }
 
 // The bf16 pairs of a dword of eight codes, times the scale: bits 23 to 30 of it alone count, 255 there gives NaN.
@@ -223,6 +224,7 @@ struct Window {
   int slab;   // which slab (16 tokens of one KV head; 4 KiB at D = 128 in bf16), counted from the pool's start; 0 when not read
   int meta;   // bits 0-7 valid tokens (0..16), then the kMeta flags; with a span, bits 16-31 the tokens that are seen
   int seg;    // s * Hkv + kvh: the segment, whose first query/output row is seg * G
+  int scales;   // with a scale for each block: the byte of K, from bit 8 that of V
 };
 // A position of the stream: block b of the nb blocks of request s, KV head kvh.
 struct Place {
@@ -295,6 +297,7 @@ template <int kD, bool kFp8, typename Layers, bool kLarge>
 __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnLaunch a, Layers layers) {
   constexpr bool kFp4 = std::is_base_of_v<Fp4Pools, Layers>;   // kFp8 is set with it: pools that are widened
   constexpr bool kSpan = std::is_base_of_v<SpanLayer, Layers>;
+  constexpr bool kBlk = std::is_base_of_v<BlockScales, Layers>;   // kFp8 is set with it, too
   typedef std::conditional_t<kFp4, Fp4Dim<kD>, Dim<kD, kFp8>> DD;
   typedef typename KLoadOf<kD, kFp4>::Type KReg;  // one K load as it arrives
   typedef typename DD::VReg VReg;                 // one V load
@@ -505,6 +508,13 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     return Place{s, kvh + more, more ? b - r.nb : b, r.nb};
   };
   const int upb_bits = 31 - __clz(a.upb);
+  [[maybe_unused]] auto scales_of = [&](int id, int kvh) -> int {
+    if constexpr (kBlk) {
+      const int64_t at = (int64_t)id * scale_row_bytes(Hkv) + kvh;
+      return layers.k_scales[at] | layers.v_scales[at] << 8;
+    }
+    return 0;
+  };
   // Descriptors of stream indices jb .. jb+63 of this share.
   auto describe = [&](int jb) __attribute__((always_inline)) -> Window {
     const int j = jb + lane;
@@ -535,6 +545,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     if (!mapped) ntok = 0;
     refused += __popcll(__ballot(live && !mapped));
     Window d;
+    if constexpr (kBlk) d.scales = mapped ? scales_of(id, kvh) : 0;
     d.slab = mapped ? ((id * Hkv + kvh) << upb_bits) + (u - (tb << upb_bits)) : 0;
     bool last = (b + 1 == nb) || (j + 1 == nshare);
     if (__any(nb > bpp)) last |= (unsigned)(b + 1) % (unsigned)bpp == 0;
@@ -561,6 +572,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       const bool ends = b + 1 == units_of(whole_len);
       const bool last = ends || ((b + 1) % bpp == 0) || (lane + 1 == nshare);
       Window d;
+      if constexpr (kBlk) d.scales = mapped ? scales_of(id, blockIdx.x) : 0;
       d.slab = mapped ? (((id * Hkv + (int)blockIdx.x) << upb_bits) + (u - (tb << upb_bits))) : 0;
       d.meta = !live ? 0
                      : (mapped ? min(kBlockTokens, whole_len - kBlockTokens * u) : 0) | (last ? kMetaLast : 0) |
@@ -574,6 +586,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     const bool mapped = live && (unsigned)id < (unsigned)a.NB;
     refused += __popcll(__ballot(live && !mapped));
     Window d;
+    if constexpr (kBlk) d.scales = mapped ? scales_of(id, blockIdx.x) : 0;
     d.slab = mapped ? (((id * Hkv + (int)blockIdx.x) << upb_bits) + (b - (tb << upb_bits))) : 0;
     const bool ends = 16 * (b + 1) >= whole_len;
     const bool last = ends || ((b + 1) % bpp == 0) || (lane + 1 == nshare);
@@ -586,7 +599,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   Window dA;
   if constexpr (kWhole) dA = describe_whole();
   else dA = describe(0);
-  Window dB = {0, 0, 0};   // described when the first blocks have been consumed (below)
+  Window dB = {};   // described when the first blocks have been consumed (below)
   int jbase = 0;           // stream index of window A's first block
 
   const int64_t slab_bytes = kFp4 ? fp4_tile_bytes(kD) : (int64_t)kBlockTokens * kD * kElemBytes;  // one (block, KV head) slab
@@ -614,6 +627,13 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   };
   auto block_at = [&](int j) {
     return Block{__builtin_amdgcn_readlane(dA.slab, j - jbase), __builtin_amdgcn_readlane(dA.meta, j - jbase)};
+  };
+  // With a scale for each block: those of the block that is consumed next.  Read from the window once its loads are out, so that the first ones
+  // do not wait for scales.
+  [[maybe_unused]] int scales_at = 0;
+  auto block_scales = [&](int j) {
+    if constexpr (kBlk) return __builtin_amdgcn_readlane(dA.scales, j - jbase);
+    else return 0;
   };
   // The loads of a block, nontemporal: the stream is read once and must not allocate in the
   // caches it passes through.  The loads are unconditional so that every wait in the loop knows
@@ -829,11 +849,12 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       // token and dims as in a bf16 pool, one byte each.
       u32x4 k[kKSteps];
       VOp v[kVLoads];
+      const float k_scale = kBlk ? scale_of(scales_at & 0xff) : 1.f, v_scale = kBlk ? scale_of(scales_at >> 8) : 1.f;
 #pragma unroll
       for (int jj = 0; jj < kKLoads; ++jj) {
         const u32x4 x = kraw[jj];
         if constexpr (kFp8) {
-          const u32x2 y[4] = {widen_e4m3x4(x.x), widen_e4m3x4(x.y), widen_e4m3x4(x.z), widen_e4m3x4(x.w)};
+          const u32x2 y[4] = {widen_e4m3x4(x.x, k_scale), widen_e4m3x4(x.y, k_scale), widen_e4m3x4(x.z, k_scale), widen_e4m3x4(x.w, k_scale)};
           k[2 * jj] = u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
           k[2 * jj + 1] = u32x4{y[2].x, y[2].y, y[3].x, y[3].y};
         } else {
@@ -845,9 +866,9 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
         if constexpr (!kFp8) {
           v[e] = vraw[e];
         } else if constexpr (kD == 64) {
-          v[e] = widen_e4m3x4(vraw[e]);
+          v[e] = widen_e4m3x4(vraw[e], v_scale);
         } else {
-          const u32x2 a2 = widen_e4m3x4(vraw[e].x), b2 = widen_e4m3x4(vraw[e].y);
+          const u32x2 a2 = widen_e4m3x4(vraw[e].x, v_scale), b2 = widen_e4m3x4(vraw[e].y, v_scale);
           v[e] = VOp{a2.x, a2.y, b2.x, b2.y};
         }
       }
@@ -1047,6 +1068,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     issue_k(kbuf[0], at, 0, kKLoads);
     if (!kLate) issue_v(vbuf[0], at);
     if (!kWhole) load_q(__builtin_amdgcn_readlane(dA.seg, 0));
+    scales_at = block_scales(0);
   }
   if (wave == 0 && kLeavesWords) {
     // Word for the reduce pass, while the first loads are on their way: the segment of the workgroup's
@@ -1093,7 +1115,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       if (!kWhole && !walk.described) {   // window A has just been begun: the one after it is described now
         walk.described = true;
         if (jbase + kWindow < nshare) dB = describe(jbase + kWindow);
-        else dB = Window{0, 0, 0};
+        else dB = Window{};
       }
     }
   }
@@ -1116,6 +1138,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
         issue_k(knext, next, 0, kKLoads);
         issue_v(vnext, next);
       }
+      const int scales_next = block_scales(j + i + 1);
       if (kTwoBlocks) arrived_k(k);
       if (j + i < nshare) {
         take_q(at.meta);
@@ -1125,10 +1148,11 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       }
       if (kLate) issue_k(knext, next, kNextK, kKLoads);
       at = next;
+      scales_at = scales_next;
     }
     if (!kWhole && j == jbase) {   // window A has just been begun: the one after it is described now
       if (jbase + kWindow < nshare) dB = describe(jbase + kWindow);
-      else dB = Window{0, 0, 0};
+      else dB = Window{};
     }
   }
   store_staged();
@@ -1168,7 +1192,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
     issue_k(kbuf[0], at, 0, kKLoads);
     if (!kLate) issue_v(vbuf[0], at);
     load_q(__builtin_amdgcn_readlane(dA.seg, 0));
-    dB = Window{0, 0, 0};
+    dB = Window{};
     seg_open = false;
     ends_flags = left = right = 0;
   }

@@ -1,0 +1,184 @@
+// New tokens into e4m3 pools with a scale for each block and KV head, for gfx950.
+//
+//   scale 2^e, e the least from -117 to 119 with no |x| > 448 * 2^e among the call's values of a block and KV head; a block that held tokens keeps a
+//   larger one, and if its own is smaller the rows that it held are rounded to 2^e;  byte = e4m3(x / scale)
+//
+// Scales are powers of two: dividing by one is exact, so that a value is rounded once, and again only where a block's scale grows past its subnormal
+// ones.  The rows of a block and KV head, of K or of V, are D / 8 lanes' own, which turn them (kv_rope.h), find the largest among them without
+// leaving registers, and write: no workgroup waits for another, nothing is read twice up to kHeld rows.
+#include "kv_rope.h"
+
+namespace pkv {
+namespace {
+
+constexpr int kHeld = 8;   // rows that a lane keeps, as it turned them
+
+// The part of a request's new tokens that falls into one block: positions [from, to) of request s, `token` being the first one's.
+struct InBlock {
+  int s, from, to, token;
+};
+// Slots: request s has slots token_starts[s] / B + 2 * s and on, which are enough wherever its tokens begin in a block.  For all lanes the same.
+__device__ __forceinline__ InBlock in_block(const RopeLaunch& a, int slot) {
+  typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
+  int s = slot, start = slot, end = slot + 1, k = 0;
+  if (a.token_starts) {
+    // one look of 64 lanes up to 63 requests, else two, kMaxSeqs being 32 times 64
+    const int lane = threadIdx.x & 63, step = (a.S >> 6) + 1;
+    auto begin = [&](int i) { return min(max(a.token_starts[min(i, a.S)], 0), a.T); };
+    int base = 0;
+    if (step > 1) {
+      const int i = lane * step;
+      base = max(__popcll(__ballot(i < a.S && (begin(i) >> a.log_block) + 2 * i <= slot)) - 1, 0) * step;
+    }
+    const int j = base + lane, at = begin(j);
+    const int found = __popcll(__ballot(j < a.S && lane < 63 && (at >> a.log_block) + 2 * j <= slot)) - 1;
+    if (found < 0) return {0, 0, 0, 0};
+    s = base + found;
+    start = __builtin_amdgcn_readlane(at, found);
+    end = __builtin_amdgcn_readlane(at, found + 1);
+    k = slot - (start >> a.log_block) - 2 * s;
+  }
+  const int L = min(max(*(ScalarLoad)(a.context_lens + s), 0), a.max_ctx), n = end - start;
+  if (n <= 0) return {0, 0, 0, 0};
+  const int first = max(L - n, 0);   // tokens before position 0 have none
+  const int block = (first >> a.log_block) + k;
+  const int from = max(first, block << a.log_block), to = min(L, (block + 1) << a.log_block);
+  return {s, from, to, end - (L - from)};
+}
+
+__device__ __forceinline__ int pack_e4m3(float w, float x, float y, float z) {
+  return __builtin_amdgcn_cvt_pk_fp8_f32(y, z, __builtin_amdgcn_cvt_pk_fp8_f32(w, x, 0, false), true);
+}
+
+struct Scales {
+  uint8_t *k, *v;
+};
+
+// Workgroups [0, append_groups): `parts` to a slot, each with blockDim.x / (D / 8) rows of heads, keys first and then values.  Those behind them, in a
+// step's launch, have the queries: `q_parts` to a token.
+template <int kD>
+__global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, Scales scales, int parts, int append_groups, int q_parts) {
+  typedef Lane<kD, 1> L;
+  constexpr int kLanes = L::kLanes;
+  const L lane(a);
+  const int groups = blockDim.x / kLanes;
+  if ((int)blockIdx.x >= append_groups) {
+    const int at = blockIdx.x - append_groups, token = at / q_parts;
+    const int r = (at - token * q_parts) * groups + threadIdx.x / kLanes;
+    const Raw raw = lane.ask(a, token, min(r, a.Hq - 1));
+    const TokenAt t = token_at(a, token);
+    if (t.position < 0 || r >= a.Hq) return;
+    f32x4 cs = {}, sn = {};
+    lane.ask_turn(a, t.position, cs, sn);
+    lane.finish(a, token, r, t.position, 0, raw, cs, sn);
+    return;
+  }
+  const int slot = blockIdx.x / parts, part = blockIdx.x - slot * parts;
+  const InBlock at = in_block(a, slot);
+  const int count = at.to - at.from;
+  if (count <= 0) return;
+  const int id = a.block_tables[(int64_t)at.s * a.MAXB + (at.from >> a.log_block)];
+  if ((unsigned)id >= (unsigned)a.NB) {   // never follow a corrupt id
+    if (part == 0 && threadIdx.x == 0 && a.id_faults) atomicAdd(a.id_faults, 1);
+    return;
+  }
+  const int kind = part * groups + threadIdx.x / kLanes;
+  if (kind >= 2 * a.Hkv) return;
+  const bool is_v = kind >= a.Hkv;
+  const int head = is_v ? kind - a.Hkv : kind;
+  const int slot0 = at.from & ((1 << a.log_block) - 1);   // rows before it were there
+  uint8_t* scale_at = (is_v ? scales.v : scales.k) + (int64_t)id * scale_row_bytes(a.Hkv) + head;
+  char* block = (char*)(is_v ? a.v_pool : a.k_pool) + (((int64_t)id * a.Hkv + head) << a.log_block) * kD;
+  const int held = slot0 ? min(max((int)*scale_at, 10), 246) : 0;
+
+  float x[kHeld][8];
+  auto ask = [&](int from) {
+    Raw raw[kHeld];
+    f32x4 cs[kHeld] = {}, sn[kHeld] = {};
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) raw[i] = lane.ask(a, at.token + min(from + i, count - 1), a.Hq + kind);
+    if (!is_v) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i) lane.ask_turn(a, at.from + min(from + i, count - 1), cs[i], sn[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) lane.template finish<true>(a, 0, a.Hq + kind, 0, 0, raw[i], cs[i], sn[i], &x[i]);
+  };
+  uint32_t most = 0;   // of the magnitudes' bits, of finite values
+  for (int from = 0; from < count; from += kHeld) {
+    ask(from);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t size = __float_as_uint(x[i][e]) & 0x7fffffffu;
+        most = max(most, size < 0x7f800000u ? size : 0u);
+      }
+  }
+#pragma unroll
+  for (int step = 1; step < kLanes; step <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, step));
+  // 448 is 1.75 * 2^8
+  const int need = min(max((int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u), 10), 246), byte = max(held, need);
+  if (slot0 && byte > held) {
+    // what the block held, rounded to the larger scale; factors below 2^-100 leave zeros as that does
+    const float factor = __uint_as_float((uint32_t)(127 - min(byte - held, 100)) << 23);
+    for (int t = 0; t < slot0; ++t) {
+      u32x2* row = (u32x2*)(block + t * kD + 8 * lane.n);
+      const u32x2 w = *row;
+      u32x2 y;
+#pragma unroll
+      for (int z = 0; z < 2; ++z)
+        y[z] = pack_e4m3(__builtin_amdgcn_cvt_f32_fp8(w[z], 0) * factor, __builtin_amdgcn_cvt_f32_fp8(w[z], 1) * factor,
+                         __builtin_amdgcn_cvt_f32_fp8(w[z], 2) * factor, __builtin_amdgcn_cvt_f32_fp8(w[z], 3) * factor);
+      *row = y;
+    }
+  }
+  if (lane.n == 0 && (!slot0 || byte != held)) *scale_at = (uint8_t)byte;
+  const float inverse = __uint_as_float((uint32_t)(254 - byte) << 23);
+  const int p0 = choose(is_v, lane.v0, lane.p0), p1 = choose(is_v, lane.v1, lane.p1);
+  for (int from = 0; from < count; from += kHeld) {
+    if (count > kHeld) ask(from);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      if (from + i >= count) break;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = to_range(x[i][e] * inverse);
+      char* row = block + (slot0 + from + i) * kD;
+      __builtin_nontemporal_store(pack_e4m3(y[0], y[1], y[2], y[3]), (int*)(row + p0));
+      __builtin_nontemporal_store(pack_e4m3(y[4], y[5], y[6], y[7]), (int*)(row + p1));
+    }
+  }
+}
+
+template <int kD>
+hipError_t launch_dim(const RopeLaunch& a, const Scales& scales, bool queries, hipStream_t stream) {
+  constexpr int kLanes = kD / 8;
+  const int kinds = 2 * a.Hkv;
+  int threads = kinds * kLanes < kThreads ? (kinds * kLanes + 63) / 64 * 64 : kThreads;
+  const int groups = threads / kLanes, parts = (kinds + groups - 1) / groups, q_parts = (a.Hq + groups - 1) / groups;
+  const int slots = a.token_starts ? (a.T >> a.log_block) + 2 * a.S : a.S;
+  const int64_t append_groups = (int64_t)slots * parts, all = append_groups + (queries ? (int64_t)a.T * q_parts : 0);
+  if (all * threads > UINT32_MAX) return hipErrorInvalidValue;   // a launch has fewer lanes
+  hipLaunchKernelGGL((kv_append_blk_kernel<kD>), dim3((unsigned)all), dim3(threads), 0, stream, a, scales, parts, (int)append_groups, q_parts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_append_blk(const RopeLaunch& a, uint8_t* k_scales, uint8_t* v_scales, hipStream_t stream) {
+  const Scales scales = {k_scales, v_scales};
+  const bool queries = a.q_out != nullptr, many = a.T >= 1024, with_them = queries && !many;
+  const hipError_t e = a.D == 64    ? launch_dim<64>(a, scales, with_them, stream)
+                       : a.D == 128 ? launch_dim<128>(a, scales, with_them, stream)
+                       : a.D == 256 ? launch_dim<256>(a, scales, with_them, stream)
+                                    : hipErrorInvalidValue;
+  if (e != hipSuccess || !queries || !many) return e;
+  RopeLaunch rest = a;   // queries alone, several rows of a token to a lane
+  rest.Hkv = 0;
+  rest.kv_fp8 = 1;
+  rest.id_faults = nullptr;
+  return launch_kv_rope(rest, stream);
+}
+
+}  // namespace pkv

@@ -39,7 +39,7 @@ int static_scratch(void** out) {
 
 extern "C" {
 
-int pkv_version(void) { return 1004; }
+int pkv_version(void) { return 1005; }
 
 const char* pkv_status_string(int status) {
   switch (status) {

@@ -23,9 +23,12 @@ float inverse_of(float scale) { return scale >= 0x1p-60f && scale <= 0x1p60f ? 1
 constexpr int64_t kMaxTokens = ((int64_t)1 << 24) - 1;   // a workgroup of 256 lanes for each in one dimension of a launch
 constexpr int64_t kMaxStride = (int64_t)1 << 31;
 
-int rope_append(const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm, const float* cos_sin, void* q_out,
-                void* k_pool, void* v_pool, const int32_t* block_tables, const int32_t* context_lens, const int32_t* token_starts, int kv_fp8,
-                float k_scale, float v_scale, const pkv_rope_shape* rope, const pkv_attn_shape* shape, void* stream) {
+// Checks a call's arguments and fills its launch; `empty`: there is nothing to do.  With `no_queries` q and q_out may both be missing.
+int prepare_rope(const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm, const float* cos_sin, void* q_out,
+                 void* k_pool, void* v_pool, const int32_t* block_tables, const int32_t* context_lens, const int32_t* token_starts, int kv_fp8,
+                 float k_scale, float v_scale, const pkv_rope_shape* rope, const pkv_attn_shape* shape, bool no_queries, RopeLaunch* launch,
+                 bool* empty) {
+  *empty = false;
   if (!rope) return PKV_ERR_NULL;
   Geometry g;
   const int rc = check_shape(shape, &g);
@@ -46,8 +49,10 @@ int rope_append(const void* q, const void* k, const void* v, const void* q_norm,
     if (s % 8 != 0) return PKV_ERR_ALIGN;
   }
   if (!token_starts && T != shape->num_seqs) return PKV_ERR_SHAPE;
-  if (T == 0 || shape->num_seqs == 0) return PKV_OK;
-  if (!q || !k || !v || !q_out || !k_pool || !v_pool || !block_tables || !context_lens || (R > 0 && !cos_sin)) return PKV_ERR_NULL;
+  *empty = T == 0 || shape->num_seqs == 0;
+  if (*empty) return PKV_OK;
+  no_queries = no_queries && !q && !q_out;
+  if (((!q || !q_out) && !no_queries) || !k || !v || !k_pool || !v_pool || !block_tables || !context_lens || (R > 0 && !cos_sin)) return PKV_ERR_NULL;
   if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(q_out) || misaligned16(k_pool) || misaligned16(v_pool) ||
       misaligned16(q_norm) || misaligned16(k_norm) || misaligned16(cos_sin) || misaligned4(block_tables) || misaligned4(context_lens) ||
       misaligned4(token_starts))
@@ -55,10 +60,10 @@ int rope_append(const void* q, const void* k, const void* v, const void* q_norm,
   // a row of q is read by the lanes that write it, so it may be written in place; no other row may be written before it is read
   const Range out = rows_at(q_out, T, q_row, q_row);
   const bool in_place = q_out == q && strides[0] == q_row;
-  if ((!in_place && meet(out, rows_at(q, T, strides[0], q_row))) || meet(out, rows_at(k, T, strides[1], kv_row)) ||
-      meet(out, rows_at(v, T, strides[2], kv_row)))
+  if (!no_queries && ((!in_place && meet(out, rows_at(q, T, strides[0], q_row))) || meet(out, rows_at(k, T, strides[1], kv_row)) ||
+                      meet(out, rows_at(v, T, strides[2], kv_row))))
     return PKV_ERR_SHAPE;
-  RopeLaunch a;
+  RopeLaunch& a = *launch;
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
   a.v = static_cast<const uint16_t*>(v);
@@ -92,12 +97,45 @@ int rope_append(const void* q, const void* k, const void* v, const void* q_norm,
   a.log_block = __builtin_ctz(shape->block_size);
   a.max_ctx = g.max_ctx;
   a.NB = (int)shape->num_pool_blocks;
+  return PKV_OK;
+}
+
+int rope_append(const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm, const float* cos_sin, void* q_out,
+                void* k_pool, void* v_pool, const int32_t* block_tables, const int32_t* context_lens, const int32_t* token_starts, int kv_fp8,
+                float k_scale, float v_scale, const pkv_rope_shape* rope, const pkv_attn_shape* shape, void* stream) {
+  RopeLaunch a;
+  bool empty;
+  const int rc = prepare_rope(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens, token_starts, kv_fp8, k_scale,
+                              v_scale, rope, shape, false, &a, &empty);
+  if (rc != PKV_OK || empty) return rc;
   return launch_status(launch_kv_rope(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // namespace
 
 extern "C" {
+
+int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm, const float* cos_sin, void* q_out,
+                          void* k_pool, void* v_pool, uint8_t* k_scales, uint8_t* v_scales, const int32_t* block_tables,
+                          const int32_t* context_lens, const int32_t* token_starts, const pkv_rope_shape* rope, const pkv_attn_shape* shape,
+                          void* stream) {
+  RopeLaunch a;
+  bool empty;
+  const int rc = prepare_rope(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens, token_starts, kBlkPools, 1.f,
+                              1.f, rope, shape, true, &a, &empty);
+  if (rc != PKV_OK || empty) return rc;
+  if (!k_scales || !v_scales) return PKV_ERR_NULL;
+  if (misaligned16(k_scales) || misaligned16(v_scales)) return PKV_ERR_ALIGN;
+  return launch_status(launch_kv_append_blk(a, k_scales, v_scales, static_cast<hipStream_t>(stream)));
+}
+
+int kv_append_fp8blk(const void* k_new, const void* v_new, void* k_pool, void* v_pool, uint8_t* k_scales, uint8_t* v_scales,
+                     const int32_t* block_tables, const int32_t* context_lens, const pkv_attn_shape* shape, void* stream) {
+  if (!shape) return PKV_ERR_NULL;
+  const pkv_rope_shape rows = {shape->num_seqs, 0, 0, 0, 0, 0, 0, 0.f};   // nothing rotated, no gaps
+  return kv_rope_append_fp8blk(nullptr, k_new, v_new, nullptr, nullptr, nullptr, nullptr, k_pool, v_pool, k_scales, v_scales, block_tables,
+                               context_lens, nullptr, &rows, shape, stream);
+}
 
 int kv_rope_append(const void* q, const void* k, const void* v, const void* q_norm, const void* k_norm, const float* cos_sin, void* q_out,
                    void* k_pool, void* v_pool, const int32_t* block_tables, const int32_t* context_lens, const int32_t* token_starts,

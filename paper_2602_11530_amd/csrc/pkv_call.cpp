@@ -85,6 +85,14 @@ struct Number32 : Number {   // those that do not fit are left to the caller
     return !overflow && x == (int32_t)x;
   }
 };
+struct Number64 : Number {
+  bool take(PyObject* o) {
+    int overflow = 0;
+    if (!PyLong_Check(o)) return false;
+    v = PyLong_AsLongLongAndOverflow(o, &overflow);
+    return !overflow;
+  }
+};
 struct Stream {   // a handle, an object that has one, or None for the current device's current stream
   void* p = nullptr;
   bool take(PyObject* o) {
@@ -124,6 +132,7 @@ std::tuple<AnyPointer> c_args(const Address& a) { return {AnyPointer{a.p}}; }
 std::tuple<AnyPointer, size_t> c_args(const Workspace& a) { return {AnyPointer{a.p}, a.bytes}; }
 std::tuple<int64_t> c_args(const Number& a) { return {a.v}; }
 std::tuple<float> c_args(const Real& a) { return {a.v}; }
+std::tuple<int64_t> c_args(const Number64& a) { return {a.v}; }
 std::tuple<int32_t> c_args(const Number32& a) { return {(int32_t)a.v}; }
 template <typename C, PyObject** kType>
 std::tuple<const C*> c_args(const Struct<C, kType>& a) { return {(const C*)a.view.buf}; }
@@ -172,6 +181,12 @@ using SpanFp4 = Entry<__LINE__, decltype(paged_decode_attn_window_fp4kv), T, T, 
 using RopeBf16 = Entry<__LINE__, decltype(kv_rope_append), T, T, T, T, T, T, T, T, T, T, T, T, Rope, Shape, Stream>;
 using RopeFp8 = Entry<__LINE__, decltype(kv_rope_append_fp8), T, T, T, T, T, T, T, T, T, T, T, T, Real, Real, Rope, Shape, Stream>;
 using RopeFp4 = Entry<__LINE__, decltype(kv_rope_append_fp4), T, T, T, T, T, T, T, T, T, T, T, T, Rope, Shape, Stream>;
+using AppendBlk = Entry<__LINE__, decltype(kv_append_fp8blk), T, T, T, T, T, T, T, T, Shape, Stream>;
+using AttnBlk = Entry<__LINE__, decltype(paged_decode_attn_fp8blk), T, T, T, T, T, T, T, Real, T, Shape, Workspace, Stream>;
+using RopeBlk = Entry<__LINE__, decltype(kv_rope_append_fp8blk), T, T, T, T, T, T, T, T, T, T, T, T, T, T, Rope, Shape, Stream>;
+using Prompt = Entry<__LINE__, decltype(paged_prompt_attn), T, T, T, T, T, T, Number64, Real, T, Shape, Workspace, Stream>;
+using PromptFp8 = Entry<__LINE__, decltype(paged_prompt_attn_fp8kv), T, T, T, T, T, T, Number64, Real, Real, Real, T, Shape, Workspace, Stream>;
+using PromptBlk = Entry<__LINE__, decltype(paged_prompt_attn_fp8blk), T, T, T, T, T, T, T, T, Number64, Real, T, Shape, Workspace, Stream>;
 using Gather = Entry<__LINE__, decltype(kv_blocks_gather), T, T, T, Number, Number, Number, Stream>;
 using Scatter = Entry<__LINE__, decltype(kv_blocks_scatter), T, T, T, Number, Number, Number, Stream>;
 using Move = Entry<__LINE__, decltype(kv_blocks_move), T, T, T, T, Number, Number, Number, Number, Stream>;
@@ -209,6 +224,12 @@ PyObject* setup(PyObject*, PyObject* args) {
   set_address<RopeBf16>(addresses, "kv_rope_append");
   set_address<RopeFp8>(addresses, "kv_rope_append_fp8");
   set_address<RopeFp4>(addresses, "kv_rope_append_fp4");
+  set_address<AppendBlk>(addresses, "kv_append_fp8blk");
+  set_address<AttnBlk>(addresses, "paged_decode_attn_fp8blk");
+  set_address<RopeBlk>(addresses, "kv_rope_append_fp8blk");
+  set_address<Prompt>(addresses, "paged_prompt_attn");
+  set_address<PromptFp8>(addresses, "paged_prompt_attn_fp8kv");
+  set_address<PromptBlk>(addresses, "paged_prompt_attn_fp8blk");
   const std::pair<PyObject**, PyObject*> keep[] = {
       {&g_shape_type, shape}, {&g_rope_type, rope}, {&g_initialized, initialized}, {&g_device, device}, {&g_raw_stream, raw}};
   for (auto& k : keep) {
@@ -244,6 +265,12 @@ PyMethodDef methods[] = {
     method<RopeBf16>("kv_rope_append"),
     method<RopeFp8>("kv_rope_append_fp8"),
     method<RopeFp4>("kv_rope_append_fp4"),
+    method<AppendBlk>("kv_append_fp8blk"),
+    method<AttnBlk>("paged_decode_attn_fp8blk"),
+    method<RopeBlk>("kv_rope_append_fp8blk"),
+    method<Prompt>("paged_prompt_attn"),
+    method<PromptFp8>("paged_prompt_attn_fp8kv"),
+    method<PromptBlk>("paged_prompt_attn_fp8blk"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pkv_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -165,7 +165,9 @@ struct AttnLayer {
   uint16_t* out;
 };
 constexpr int kMaxLaunchLayers = 8;
-constexpr int kFp4Pools = 2;
+// AttnLaunch::kv_fp8: pools of E2M1 tiles, and e4m3 pools with a scale for each block and KV head, a row of scale bytes for each block.
+constexpr int kFp4Pools = 2, kBlkPools = 3;
+__host__ __device__ constexpr int scale_row_bytes(int Hkv) { return (Hkv + 15) & ~15; }
 
 struct AttnLaunch {
   AttnLayer layer;
@@ -177,7 +179,7 @@ struct AttnLaunch {
   int short_blocks;    // see short_segment()
   float scale_log2e;   // softmax scale x log2(e) (x the K pool's scale for an e4m3 pool)
   float out_scale;     // applied to the normalised row: 1, or the V pool's scale
-  int kv_fp8;          // the pools hold one-byte e4m3 values (1), E2M1 tiles (kFp4Pools)
+  int kv_fp8;          // the pools hold one-byte e4m3 values (1), E2M1 tiles (kFp4Pools), kBlkPools
   int32_t* id_faults;  // optional device counter of refused block ids (nullptr: not reported)
   int S, Hq, Hkv, G, MAXB;
   int D;           // head dimension: 64, 128 or 256
@@ -236,6 +238,12 @@ struct SpanLayer : OneLayer {
 struct Fp4Pools {};
 struct Fp4Layer : OneLayer, Fp4Pools {};
 struct Fp4SpanLayer : SpanLayer, Fp4Pools {};
+// e4m3 pools with a scale for each block and KV head.
+struct BlockScales {
+  const uint8_t *k_scales, *v_scales;
+};
+struct BlkLayer : OneLayer, BlockScales {};
+struct WholeBlkLayer : BlkLayer, GroupPerSegment {};
 struct WholeSpanLayer : SpanLayer, GroupPerSegment {};
 struct WholeFp4Layer : Fp4Layer, GroupPerSegment {};
 struct WholeFp4SpanLayer : Fp4SpanLayer, GroupPerSegment {};
@@ -318,6 +326,8 @@ inline bool short_at_128(const AttnLaunch& a) {
   const int64_t most = (int64_t)a.S * a.Hkv * ((a.max_ctx + kBlockTokens - 1) / kBlockTokens);
   return a.D == 128 && !a.kv_fp8 && most <= 16 * (int64_t)a.waves;
 }
+// The stream pass over e4m3 pools with a scale for each block and KV head.
+hipError_t launch_attn_blk(const AttnLaunch& a, const uint8_t* k_scales, const uint8_t* v_scales, hipStream_t stream);
 // The stream pass over E2M1 tiles, or for requests that see part of their context, or both.  `span`: nullptr for all of it.
 hipError_t launch_attn_span(const AttnLaunch& a, const Span* span, hipStream_t stream);
 // With LDS laid out: over tiles, and where each segment has a workgroup.
@@ -394,6 +404,37 @@ struct RopeLaunch {
   int MAXB, log_block, max_ctx, NB;
 };
 hipError_t launch_kv_rope(const RopeLaunch& a, hipStream_t stream);
+// The same into e4m3 pools with a scale for each block and KV head; q_out nullptr: no queries (kv_append_blk.hip).
+hipError_t launch_kv_append_blk(const RopeLaunch& a, uint8_t* k_scales, uint8_t* v_scales, hipStream_t stream);
+
+// Prompts: causal attention of new tokens over the paged cache (prompt_attn.hip).
+constexpr int kKeyTile = 64;       // keys that a workgroup takes at a time
+struct PromptLaunch {
+  const uint16_t* q;
+  const void *k_pool, *v_pool;
+  const uint8_t *k_scales, *v_scales;   // kBlkPools: [NB][scale_row_bytes]
+  const int32_t *block_tables, *context_lens;
+  const int32_t* token_starts;          // [S + 1]; nullptr: token s is request s's last one
+  uint16_t* out;
+  float* parts;                         // [pieces][T][Hq][D], the rows of pieces of a context
+  float* stats;                         // [pieces][T][Hq][2], their reference maxima in log2 units and sums
+  int32_t* id_faults;
+  float scale_log2e, out_scale;
+  int kv_fp8;                           // as in AttnLaunch, or kBlkPools
+  int T, S, Hq, Hkv, G, D;
+  int MAXB, log_block, max_ctx, NB;
+  int piece;                            // tiles of keys that a workgroup takes at most
+  int pieces;                           // of a context, by the bounds
+};
+// How a launch cuts its work, by what the host knows.
+struct PromptPlan {
+  int rows;         // query rows of a workgroup
+  int tokens;       // that they are of
+  int64_t slots;    // groups of that many tokens, at most
+  int piece, pieces;
+};
+PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx);
+hipError_t launch_prompt(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream);
 
 // Measurement aid: the stream pass's loads at D = 128 in bf16 with no arithmetic (see stream_probe.hip).
 hipError_t launch_stream_read_probe(const void* k_buf, const void* v_buf, uint32_t num_slabs,
