@@ -408,7 +408,6 @@ hipError_t launch_kv_rope(const RopeLaunch& a, hipStream_t stream);
 hipError_t launch_kv_append_blk(const RopeLaunch& a, uint8_t* k_scales, uint8_t* v_scales, hipStream_t stream);
 
 // Prompts: causal attention of new tokens over the paged cache (prompt_attn.hip).
-constexpr int kKeyTile = 64;       // keys that a workgroup takes at a time
 struct PromptLaunch {
   const uint16_t* q;
   const void *k_pool, *v_pool;

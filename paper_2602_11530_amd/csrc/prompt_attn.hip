@@ -25,11 +25,17 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
 
 constexpr float kLazyLog2 = 8.f;
+constexpr float kLeast = -3e38f;                  // a reference maximum before any score: finite, so that what is masked, -inf, gives weights of zero
 constexpr int kRawBuffer = 0x00020000;
-constexpr int kUnits = kKeyTile / kBlockTokens;   // of a tile
-constexpr int kWindowTiles = 64 / kUnits;         // whose units a wavefront's lanes describe
+constexpr int kMfma = 0x8, kDsRead = 0x100;       // kinds of instructions, for the scheduler
+constexpr int kReadsAhead = 6;
+// Keys of a tile.
+__host__ __device__ constexpr int prompt_keys(int D) { return D == 256 ? 32 : 64; }
 
-__host__ __device__ constexpr int prompt_waves(int D) { return D == 256 ? 4 : 8; }
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kMaxPieces = 64;                    // of a context
+// Workgroups that run on a compute unit at once, by their registers and LDS.
+constexpr int prompt_groups(int D) { return D == 64 ? 4 : D == 128 ? 2 : 1; }
 
 // A workgroup's tokens: `first` to `first + count` of the call, of request s, at position `at` and on.
 struct Tokens {
@@ -73,6 +79,12 @@ __device__ __forceinline__ u32x2 widen(uint32_t w, float scale) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, true))};
 }
 
+// 64 lanes' pieces of a buffer, zeros out of its bounds, to 1 KiB in a row of LDS from `to` on.  An opaque instruction: the compiler would wait for it
+// before every read of LDS that follows, whatever it reads.  Who asks waits for what was asked for, and meets the others, before anyone reads it.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t b, uint32_t to, int offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
+}
+
 // Places in LDS, in bytes: 16-byte piece p of key t.  K is read 16 bytes a lane, a key to a lane; V 8 bytes a lane, four keys of 64 bytes to half
 // a wavefront.  No conflicts in either, nor where they are written.
 template <int kD> __device__ __forceinline__ int k_place(int t, int p) {
@@ -87,15 +99,20 @@ template <int kD> __device__ __forceinline__ int v_place(int t, int p) {
 }
 
 template <int kD, int kFormat>
-__global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prompt_attn_kernel(PromptLaunch a, int per, int slots, uint32_t group_inverse) {
-  constexpr int kWaves = prompt_waves(kD), kThreads = kWaves * 64, kSteps = kD / 16, kTiles = kD / 32;
+__global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kernel(PromptLaunch a, int per, int slots, uint32_t group_inverse) {
+  constexpr int kSteps = kD / 16, kTiles = kD / 32;
+  constexpr int kKeyTile = prompt_keys(kD), kHalves = kKeyTile / 32;
+  constexpr int kUnits = kKeyTile / kBlockTokens;                // of a tile
+  constexpr int kWindowTiles = 64 / kUnits;                      // whose units a wavefront's lanes describe
   constexpr int kTileBytes = kKeyTile * kD * 2;
   constexpr int kElem = kFormat == 0 ? 2 : 1;
   constexpr int kSource = kKeyTile * kD * kElem / 16;            // 16-byte pieces of a tile as the pool has it
   constexpr int kLoads = (kSource + kThreads - 1) / kThreads;    // of a lane
   constexpr int kPerToken = kD * kElem / 16;
+  constexpr bool kDirect = kFormat == 0;                         // nothing to widen: from memory straight into LDS
   __shared__ __align__(16) char lds[4 * kTileBytes];             // K and V of two tiles in turn
-  __shared__ int not_finite[2];                                  // the last tile of whose V something is not finite, plus 1
+  __shared__ int first_bad[kD];                                  // the first key whose V is not finite there, of those that some row does not see
+  __shared__ int any_bad;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -120,7 +137,7 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
 
   bf16x8 q[kSteps];
   const bool negative = a.scale_log2e < 0.f;
-  const float scale = __builtin_fabsf(a.scale_log2e);
+  const float scale = fmaxf(__builtin_fabsf(a.scale_log2e), 0x1p-126f);   // masked scores stay -inf with a scale of zero, too
 #pragma unroll
   for (int jj = 0; jj < kSteps; ++jj) {
     u32x4 x = *(const u32x4*)(a.q + q_row + 16 * jj + 8 * h);
@@ -128,25 +145,33 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
     q[jj] = __builtin_bit_cast(bf16x8, x);
   }
 
-  // Units of the context: one to a lane, a window of 64 at a time and the next one ahead.
+  // Units of the context: one to a lane, a window of 64 at a time and the next one ahead.  What a load needs of its unit is worked out there, 64 units
+  // at a time, and read from the lane.
   struct Window {
-    int slab;       // 16 keys of the KV head, counted from the pool's start; -1: not to be read
+    uint64_t at;    // of the unit's K, 16 keys of the KV head
+    int bytes;      // of its rows that are there
     int scales;     // kBlkPools: of K, of V
+    uint64_t gone;  // a bit for each unit that is not there
   };
   const int log_units = a.log_block - 4;
   const int context = tok.at + tok.count;   // keys behind this are not seen
+  const uint64_t v_behind = (uint64_t)a.v_pool - (uint64_t)a.k_pool;   // of a unit's V behind its K
   int refused = 0;
   auto describe = [&](int tile) -> Window {
     const int u = kUnits * tile + lane;
-    Window w = {-1, 0};
     const bool here = u >= kUnits * from && u * kBlockTokens < context && u < kUnits * to;
     int id = -1;
     if (here) id = a.block_tables[(int64_t)tok.s * a.MAXB + (u >> log_units)];
     const bool mapped = (unsigned)id < (unsigned)a.NB;           // ids outside the pool are never followed
     refused += __popcll(__ballot(here && !mapped));
-    if (mapped) {
-      w.slab = ((id * a.Hkv + kvh) << log_units) + (u & ((1 << log_units) - 1));
-      if constexpr (kFormat == kBlkPools) {
+    Window w;
+    const int slab = mapped ? ((id * a.Hkv + kvh) << log_units) + (u & ((1 << log_units) - 1)) : 0;
+    w.at = (uint64_t)a.k_pool + (uint64_t)slab * (kBlockTokens * kD * kElem);
+    w.bytes = mapped ? min(kBlockTokens, context - u * kBlockTokens) * (kD * kElem) : 0;
+    w.gone = __ballot(!mapped);
+    w.scales = 0;
+    if constexpr (kFormat == kBlkPools) {
+      if (mapped) {
         const int64_t at = (int64_t)id * scale_row_bytes(a.Hkv) + kvh;
         w.scales = a.k_scales[at] | a.v_scales[at] << 8;
       }
@@ -156,36 +181,48 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
   int window_at = from / kWindowTiles * kWindowTiles;
   Window now = describe(window_at), then = describe(window_at + kWindowTiles);
 
+  // kDirect: the memory unit writes 64 pieces in a row to LDS, so that each lane asks for the piece whose place is its own.
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  int k_from[kLoads], v_from[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int at = (i * kThreads + threadIdx.x) % (kPerToken * kBlockTokens), t = at / kPerToken, here = at % kPerToken;
+    k_from[i] = t * (kD * kElem) + k_place<kD>(t, here) % (kD * 2);
+    v_from[i] = t * (kD * kElem) + v_place<kD>(t, here) % (kD * 2);
+  }
   // A tile on its way: out of memory into registers, from there into LDS.
   u32x4 kr[kLoads], vr[kLoads];
   float ks[kLoads], vs[kLoads];
-  uint32_t unmapped = 0;      // of the tile that was asked for last: a bit for each key's unit that is not there
-  auto ask = [&](int tile) {
+  uint32_t unmapped = 0;      // of the tile that was asked for last, a bit for each unit that is not there
+  auto ask = [&](int tile, int at_place) {
     if (tile >= window_at + kWindowTiles) {
       now = then;
       window_at += kWindowTiles;
       then = describe(window_at + kWindowTiles);
     }
     const int u0 = kUnits * (tile - window_at);
-    unmapped = 0;
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) unmapped |= (__builtin_amdgcn_readlane(now.slab, u0 + u) < 0) << u;
+    unmapped = (uint32_t)(now.gone >> u0) & ((1 << kUnits) - 1);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int piece = i * kThreads + wave * 64;                // the wavefront's first
-      const int u = piece / kPerToken / kBlockTokens;
+      const int u = u0 + piece / kPerToken / kBlockTokens;
       if (kSource % kThreads != 0 && piece >= kSource) break;
-      const int slab = __builtin_amdgcn_readlane(now.slab, u0 + u);
-      const int rows = min(kBlockTokens, context - kKeyTile * tile - kBlockTokens * u);
-      const int64_t at = (int64_t)max(slab, 0) * (kBlockTokens * kD * kElem);
-      const int bytes = slab < 0 || rows <= 0 ? 0 : rows * kD * kElem;
-      const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.k_pool + at), 0, bytes, kRawBuffer);
-      const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.v_pool + at), 0, bytes, kRawBuffer);
+      const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(now.at >> 32), u) << 32 |
+                          (uint32_t)__builtin_amdgcn_readlane((int)now.at, u);
+      const int bytes = __builtin_amdgcn_readlane(now.bytes, u);
+      const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, kRawBuffer);
+      const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)(at + v_behind), 0, bytes, kRawBuffer);
+      if constexpr (kDirect) {
+        const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * piece;
+        load_to_lds(kb, to_lds, k_from[i]);
+        load_to_lds(vb, to_lds + kTileBytes, v_from[i]);
+        continue;
+      }
       const int offset = 16 * ((piece + lane) % (kPerToken * kBlockTokens));
       kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, 0));
       vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, 0));
       if constexpr (kFormat == kBlkPools) {
-        const int both = __builtin_amdgcn_readlane(now.scales, u0 + u);
+        const int both = __builtin_amdgcn_readlane(now.scales, u);
         ks[i] = __uint_as_float((uint32_t)(both & 0xff) << 23);
         vs[i] = __uint_as_float((uint32_t)(both >> 8) << 23);
       } else {
@@ -193,12 +230,53 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
       }
     }
   };
-  auto put = [&](int tile, char* k_lds, char* v_lds, int* flag, bool look) {
+  // What is not finite in V of keys that some row may not see does not go through the matrix product, where a weight of zero does not silence it: it
+  // is held back, and the rows that see its key become NaN there in the end.
+  auto hold_back = [&](int i, int tile, int t, int p) {
+    constexpr int kEach = 16 / kElem;
+    bool bad = false;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) {
+      const uint32_t w = vr[i][z];
+      if constexpr (kFormat == 0) bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+      else bad |= (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
+    }
+    const bool all = kFormat == kBlkPools && !(vs[i] < 0x1p120f);
+    if (!bad && !all) return;
+    any_bad = 1;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int shift = 8 * kElem * (e % (4 / kElem));
+      const uint32_t mask = kFormat == 0 ? 0x7f80u : 0x7fu;
+      if (all || ((vr[i][e * kElem / 4] >> shift) & mask) == mask) {
+        atomicMin(&first_bad[kEach * p + e], kKeyTile * tile + t);
+        vr[i][e * kElem / 4] &= ~((kFormat == 0 ? 0xffffu : 0xffu) << shift);
+      }
+    }
+    if (all) vs[i] = 1.f;
+  };
+  // kDirect: what has arrived is in place; of a tile that is looked at this lane's pieces of V are read back.
+  auto arrived = [&](int tile, char* v_lds, bool look) {
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    if (!look) return;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int piece = i * kThreads + threadIdx.x;
+      if (kSource % kThreads != 0 && piece >= kSource) break;
+      u32x4* at = (u32x4*)(v_lds + 16 * piece);
+      vr[i] = *at;
+      const u32x4 was = vr[i];
+      hold_back(i, tile, piece / kPerToken, v_place<kD>(piece / kPerToken, piece % kPerToken) % (kD * 2) / 16);
+      if (vr[i].x != was.x || vr[i].y != was.y || vr[i].z != was.z || vr[i].w != was.w) *at = vr[i];
+    }
+  };
+  auto put = [&](int tile, char* k_lds, char* v_lds, bool look) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int piece = i * kThreads + threadIdx.x;
       if (kSource % kThreads != 0 && piece >= kSource) break;
       const int t = piece / kPerToken, p = piece % kPerToken;
+      if (look) hold_back(i, tile, t, p);
       if constexpr (kFormat == 0) {
         *(u32x4*)(k_lds + k_place<kD>(t, p)) = kr[i];
         *(u32x4*)(v_lds + v_place<kD>(t, p)) = vr[i];
@@ -211,21 +289,10 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
           *(u32x4*)(v_lds + v_place<kD>(t, 2 * p + z)) = u32x4{v0.x, v0.y, v1.x, v1.y};
         }
       }
-      if (look) {   // a weight of zero does not silence what is not finite
-        bool bad = false;
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          const uint32_t w = vr[i][z];
-          if constexpr (kFormat == 0) bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-          else bad |= (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
-        }
-        if constexpr (kFormat == kBlkPools) bad |= !(vs[i] < 0x1p120f);
-        if (bad) *flag = tile + 1;
-      }
     }
   };
 
-  float m = kNegInf, l = 0.f;   // of row n: the reference maximum in log2 units, this lane's part of the sum
+  float m = kLeast, l = 0.f;   // of row n: the reference maximum in log2 units, this lane's part of the sum
   f32x16 o[kTiles];             // o[d][r]: row n, dim 32*d + 8*(r / 4) + 4*h + r % 4
 #pragma unroll
   for (int d = 0; d < kTiles; ++d)
@@ -243,41 +310,46 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
     return u32x4{xx.x, xx.y, yy.x, yy.y};
   };
 
-  auto attend = [&](const char* k_lds, const char* v_lds, int tile, uint32_t gone, bool some_not_finite) __attribute__((always_inline)) {
-    f32x16 s[2];
+  auto attend = [&](const char* k_lds, const char* v_lds, int tile, uint32_t gone) __attribute__((always_inline)) {
+    f32x16 s[kHalves];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kHalves; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
 #pragma unroll
-      for (int jj = 0; jj < kSteps; ++jj) {
+    for (int jj = 0; jj < kSteps; ++jj)
+#pragma unroll
+      for (int b = 0; b < kHalves; ++b) {
         const bf16x8 k = __builtin_bit_cast(bf16x8, *(const u32x4*)(k_lds + k_place<kD>(32 * b + n, 2 * jj + h)));
         s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[jj], s[b], 0, 0, 0);
       }
-    }
-    const int key0 = kKeyTile * tile;
-    const bool edge = gone != 0 || key0 + kKeyTile - 1 > wave_from;
-    uint32_t seen[2];   // bit r: does the row see that key
-    if (edge) {
+    // some reads ahead of the products, else each waits for its own
+    __builtin_amdgcn_sched_group_barrier(kDsRead, kReadsAhead, 0);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        seen[b] = 0;
+    for (int i = 0; i < kHalves * kSteps - kReadsAhead; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMfma, kReadsAhead, 0);
+    const int key0 = kKeyTile * tile;
+    if (gone != 0 || key0 + kKeyTile - 1 > wave_from) {
+      asm volatile("");   // a branch: most tiles have nothing to mask
+#pragma unroll
+      for (int b = 0; b < kHalves; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = 32 * b + 8 * (r >> 2) + 4 * h + (r & 3);
-          const bool ok = key0 + key <= last_key && !((gone >> (2 * b + (r >> 3))) & 1);
-          seen[b] |= (uint32_t)ok << r;
-          s[b][r] = ok ? s[b][r] : kNegInf;
+          s[b][r] = key0 + key <= last_key && !((gone >> (2 * b + (r >> 3))) & 1) ? s[b][r] : kNegInf;
         }
-      }
     }
-    float most = fmaxf(s[0][0], s[1][0]);
+    float most = s[0][0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) most = fmaxf(fmaxf(most, s[0][r]), s[1][r]);
+    for (int i = 1; i + 1 < 16 * kHalves; i += 2) most = fmaxf(fmaxf(most, s[i >> 4][i & 15]), s[(i + 1) >> 4][(i + 1) & 15]);
+    most = fmaxf(most, s[kHalves - 1][15]);
     if (__any(most * scale > m + kLazyLog2)) {
       most = fmaxf(most, __shfl_xor(most, 32)) * scale;
       const float raised = fmaxf(m, most);
-      const float alpha = raised == kNegInf ? 1.f : __builtin_amdgcn_exp2f(m - raised);
+      const float alpha = __builtin_amdgcn_exp2f(m - raised);
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < kTiles; ++d)
@@ -285,72 +357,61 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
       m = raised;
     }
-    u32x4 p[4];   // weights of keys 16*step .. +15, the B operand
-    float sum[2] = {0.f, 0.f};
+    u32x4 p[2 * kHalves];   // weights of keys 16*step .. +15, the B operand
+    float sum[kHalves] = {};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < kHalves; ++b) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale, -m));
-        if (edge) w = (seen[b] >> r) & 1 ? w : 0.f;   // m may still be -inf here
-        s[b][r] = w;
-        sum[b] += w;
+        s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale, -m));
+        sum[b] += s[b][r];
       }
 #pragma unroll
       for (int z = 0; z < 8; ++z) p[2 * b + (z >> 2)][z & 3] = pack_bf16(s[b][2 * z], s[b][2 * z + 1]);
     }
-    l += sum[0] + sum[1];
-    if (__builtin_expect(edge && some_not_finite, 0)) {
-      // What is not finite in V reaches the rows that see its key and no other.  All else first, then key by key.
+    l += kHalves == 2 ? sum[0] + sum[kHalves - 1] : sum[0];
 #pragma unroll
-      for (int step = 0; step < 4; ++step) {
-#pragma unroll 1
-        for (int key = -1; key < 16; ++key) {
-          const bool mine = key < 0 || h == ((key >> 2) & 1);
-          const int element = (key & 3) + 4 * (key >> 3);
-          const bool sees = key0 + 16 * step + key <= last_key;
-#pragma unroll
-          for (int d = 0; d < kTiles; ++d) {
-            u32x4 v = v_operand(v_lds, step, d);
-#pragma unroll
-            for (int z = 0; z < 8; ++z) {
-              const uint32_t half = z & 1 ? 0xffff0000u : 0xffffu;
-              const bool finite = (v[z >> 1] & half & 0x7f807f80u) != (half & 0x7f807f80u);
-              const bool keep = key < 0 ? finite : mine && z == element && !finite;
-              v[z >> 1] &= keep ? 0xffffffffu : ~half;
-            }
-            const f32x16 zero = {};
-            const f32x16 add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p[step]), zero, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[d][r] = key < 0 || sees ? o[d][r] + add[r] : o[d][r];
-          }
-        }
-      }
-      return;
-    }
-#pragma unroll
-    for (int step = 0; step < 4; ++step)
+    for (int step = 0; step < 2 * kHalves; ++step)
 #pragma unroll
       for (int d = 0; d < kTiles; ++d)
         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v_lds, step, d)), __builtin_bit_cast(bf16x8, p[step]), o[d],
                                                        0, 0, 0);
   };
 
-  if (threadIdx.x < 2) not_finite[threadIdx.x] = 0;
+  for (int d = threadIdx.x; d < kD; d += kThreads) first_bad[d] = INT32_MAX;
+  if (threadIdx.x == 0) any_bad = 0;
   __syncthreads();
-  ask(from);
-  for (int tile = from; tile < to; ++tile) {
-    const int turn = (tile - from) & 1;
-    char *k_lds = lds + 2 * turn * kTileBytes, *v_lds = k_lds + kTileBytes;
+  ask(from, 0);
+  auto one = [&](int tile, auto at_place) __attribute__((always_inline)) {
+    constexpr int kAt = decltype(at_place)::value;
+    char *k_lds = lds + 2 * kAt * kTileBytes, *v_lds = k_lds + kTileBytes;
     const uint32_t gone = unmapped;
-    put(tile, k_lds, v_lds, not_finite + turn, kKeyTile * tile + kKeyTile - 1 > tok.at);
-    if (tile + 1 < to) ask(tile + 1);
-    __syncthreads();
-    if (!idle && kKeyTile * tile <= wave_to) attend(k_lds, v_lds, tile, gone, not_finite[turn] == tile + 1);
+    const bool look = kKeyTile * tile + kKeyTile - 1 > tok.at;
+    if constexpr (kDirect) {   // the next tile goes where all have read the one before
+      arrived(tile, v_lds, look);
+      __syncthreads();
+      if (tile + 1 < to) ask(tile + 1, 1 - kAt);
+    } else {
+      put(tile, k_lds, v_lds, look);
+      if (tile + 1 < to) ask(tile + 1, 0);
+      __syncthreads();
+    }
+    if (!idle && kKeyTile * tile <= wave_to) attend(k_lds, v_lds, tile, gone);
+  };
+  for (int tile = from; tile < to; tile += 2) {
+    one(tile, std::integral_constant<int, 0>{});
+    if (tile + 1 < to) one(tile + 1, std::integral_constant<int, 1>{});
   }
   if (a.id_faults && refused && threadIdx.x == 0) atomicAdd(a.id_faults, refused);
 
   if (!live) return;
+  if (__builtin_expect(any_bad, 0)) {
+#pragma unroll
+    for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (first_bad[32 * d + 8 * (r >> 2) + 4 * h + (r & 3)] <= last_key) o[d][r] = __builtin_nanf("");
+  }
   const float total = l + __shfl_xor(l, 32);
   if (tiles <= a.piece) {
     const float inv = inverse(total, a.out_scale);
@@ -367,7 +428,7 @@ __global__ __launch_bounds__(prompt_waves(kD) * 64, kD == 256 ? 1 : 2) void prom
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(f32x4*)(part + 32 * d + 8 * g + 4 * h) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
-    if (h == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + q_row / kD) * 2) = f32x2{m, total};
+    if (h == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + q_row / kD) * 2) = f32x2{m == kLeast ? kNegInf : m, total};
   }
 }
 
@@ -390,6 +451,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
   const int L = min(max(a.context_lens[s], 0), a.max_ctx), n = end - from;
   if (token - from < n - L) return;
   const int last = min(((token - from) / per + 1) * per, n) - 1;     // of its workgroup's tokens
+  constexpr int kKeyTile = prompt_keys(kD);
   const int tiles = (L - n + last + 1 + kKeyTile - 1) / kKeyTile;
   if (tiles <= a.piece) return;
   const int count = (tiles + a.piece - 1) / a.piece;
@@ -418,7 +480,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
 
 template <int kD, int kFormat>
 void launch(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream) {
-  const dim3 grid((unsigned)(plan.slots * a.Hkv), plan.pieces), block(prompt_waves(kD) * 64);
+  const dim3 grid((unsigned)(plan.slots * a.Hkv), plan.pieces), block(kThreads);
   hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat>), grid, block, 0, stream, a, plan.tokens, (int)plan.slots, 65536u / a.G + 1);
   if (plan.pieces > 1) {
     const int heads = 256 / (kD / 4);
@@ -436,16 +498,26 @@ void launch_format(const PromptLaunch& a, const PromptPlan& plan, hipStream_t st
 
 PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
   PromptPlan p;
-  p.rows = 32 * prompt_waves(D);
+  p.rows = 32 * kWaves;
   p.tokens = p.rows / G;
   p.slots = T / p.tokens + S;
-  const int64_t tiles = ((int64_t)max_ctx + kKeyTile - 1) / kKeyTile, groups = p.slots * Hkv;
-  const int64_t least = 8;
-  int64_t piece = groups * tiles / 1024;
-  if (piece < least) piece = least;
-  if (piece > tiles) piece = tiles > 0 ? tiles : 1;
-  p.piece = (int)piece;
-  p.pieces = (int)(tiles > 0 ? (tiles + piece - 1) / piece : 1);
+  // Few workgroups over long contexts: those are cut.  Into as many pieces as give the least time by this estimate, in us: workgroups in turns of as many
+  // as run at once, a tile 2 us (D = 128), a start 3 tiles, and the pieces' rows written and read.
+  const int64_t tiles = ((int64_t)max_ctx + prompt_keys(D) - 1) / prompt_keys(D), groups = p.slots * Hkv, at_once = 256 * prompt_groups(D);
+  const double tile_us = 2.0 * D / 128, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
+  p.piece = (int)(tiles > 0 ? tiles : 1);
+  p.pieces = 1;
+  double least = 0;
+  for (int64_t n = 1; n <= kMaxPieces && 4 * n <= tiles + 3; ++n) {
+    const int64_t piece = (tiles + n - 1) / n;
+    const double us = (double)((groups * n + at_once - 1) / at_once) * (piece + 3) * tile_us + (n > 1 ? 5 + n * join_us : 0);
+    if (n == 1 || us < least) {
+      least = us;
+      p.piece = (int)piece;
+      p.pieces = (int)((tiles + piece - 1) / piece);
+    }
+    if (groups * n > 8 * at_once) break;
+  }
   return p;
 }
 

@@ -132,8 +132,8 @@ def test_blocks_outside_the_pool(id_faults, kind):
     got = run_prompt(b, p)
     check(b, got, *plain_prompt(b, p))
     assert (got[b.starts[2]:] == 0).all()         # nothing left to see
-    # one for each unit, KV head and group of tokens (64 of them with four heads to a KV head) that meet
-    assert int(id_faults.item()) == 2 * 2 + 2 * 2
+    # one for each unit, KV head and group of tokens (32 of them with four heads to a KV head) that meet
+    assert int(id_faults.item()) == 2 * 2 * 2 + 2 * 2
 
 
 @pytest.mark.parametrize("kind", KINDS)
