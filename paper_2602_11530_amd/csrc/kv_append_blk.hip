@@ -11,7 +11,7 @@
 namespace pkv {
 namespace {
 
-constexpr int kHeld = 8;   // rows that a lane keeps, as it turned them
+constexpr int kHeld = 8;   // rows of a block that a lane has at most, as it turned them
 
 // The part of a request's new tokens that falls into one block: positions [from, to) of request s, `token` being the first one's.
 struct InBlock {
@@ -54,17 +54,18 @@ struct Scales {
   uint8_t *k, *v;
 };
 
-// Workgroups [0, append_groups): `parts` to a slot, each with blockDim.x / (D / 8) rows of heads, keys first and then values.  Those behind them, in a
-// step's launch, have the queries: `q_parts` to a token.
+// Workgroups [0, append_groups): `parts` to a slot.  D / 8 lanes have a row, `spread` times that the rows of a block and KV head, which are keys of all heads
+// and then values.  Those behind them, in a step's launch, have the queries: `q_parts` to a token.
 template <int kD>
-__global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, Scales scales, int parts, int append_groups, int q_parts) {
+__global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, Scales scales, int spread, int parts, int append_groups, int q_parts) {
   typedef Lane<kD, 1> L;
   constexpr int kLanes = L::kLanes;
+  __shared__ uint32_t most_of[kThreads / 64];   // of each wavefront, where a head's rows are more than one's
   const L lane(a);
-  const int groups = blockDim.x / kLanes;
+  const int group = threadIdx.x / kLanes;
   if ((int)blockIdx.x >= append_groups) {
     const int at = blockIdx.x - append_groups, token = at / q_parts;
-    const int r = (at - token * q_parts) * groups + threadIdx.x / kLanes;
+    const int r = (at - token * q_parts) * ((int)blockDim.x / kLanes) + group;
     const Raw raw = lane.ask(a, token, min(r, a.Hq - 1));
     const TokenAt t = token_at(a, token);
     if (t.position < 0 || r >= a.Hq) return;
@@ -82,47 +83,54 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
     if (part == 0 && threadIdx.x == 0 && a.id_faults) atomicAdd(a.id_faults, 1);
     return;
   }
-  const int kind = part * groups + threadIdx.x / kLanes;
-  if (kind >= 2 * a.Hkv) return;
-  const bool is_v = kind >= a.Hkv;
-  const int head = is_v ? kind - a.Hkv : kind;
+  const int kinds = blockDim.x / (kLanes * spread);
+  const int kind = part * kinds + group / spread, mine = group % spread;
+  const bool live = kind < 2 * a.Hkv;
+  const int of = min(kind, 2 * a.Hkv - 1);   // lanes without a head go along
+  const bool is_v = of >= a.Hkv;
+  const int head = is_v ? of - a.Hkv : of;
   const int slot0 = at.from & ((1 << a.log_block) - 1);   // rows before it were there
   uint8_t* scale_at = (is_v ? scales.v : scales.k) + (int64_t)id * scale_row_bytes(a.Hkv) + head;
   char* block = (char*)(is_v ? a.v_pool : a.k_pool) + (((int64_t)id * a.Hkv + head) << a.log_block) * kD;
   const int held = slot0 ? min(max((int)*scale_at, 10), 246) : 0;
 
+  // this lane's rows: `mine`, `mine` + spread and on, at most kHeld of them
   float x[kHeld][8];
-  auto ask = [&](int from) {
+  {
     Raw raw[kHeld];
     f32x4 cs[kHeld] = {}, sn[kHeld] = {};
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) raw[i] = lane.ask(a, at.token + min(from + i, count - 1), a.Hq + kind);
+    for (int i = 0; i < kHeld; ++i) raw[i] = lane.ask(a, at.token + min(mine + i * spread, count - 1), a.Hq + of);
     if (!is_v) {
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) lane.ask_turn(a, at.from + min(from + i, count - 1), cs[i], sn[i]);
+      for (int i = 0; i < kHeld; ++i) lane.ask_turn(a, at.from + min(mine + i * spread, count - 1), cs[i], sn[i]);
     }
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) lane.template finish<true>(a, 0, a.Hq + kind, 0, 0, raw[i], cs[i], sn[i], &x[i]);
-  };
-  uint32_t most = 0;   // of the magnitudes' bits, of finite values
-  for (int from = 0; from < count; from += kHeld) {
-    ask(from);
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t size = __float_as_uint(x[i][e]) & 0x7fffffffu;
-        most = max(most, size < 0x7f800000u ? size : 0u);
-      }
+    for (int i = 0; i < kHeld; ++i) lane.template finish<true>(a, 0, a.Hq + of, 0, 0, raw[i], cs[i], sn[i], &x[i]);
   }
+  uint32_t most = 0;   // of the magnitudes' bits, of finite values
 #pragma unroll
-  for (int step = 1; step < kLanes; step <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, step));
+  for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t size = __float_as_uint(x[i][e]) & 0x7fffffffu;
+      most = max(most, size < 0x7f800000u ? size : 0u);
+    }
+  const int lanes = kLanes * spread;
+  for (int step = 1; step < min(lanes, 64); step <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, step));
+  if (lanes > 64) {
+    if ((threadIdx.x & 63) == 0) most_of[threadIdx.x >> 6] = most;
+    __syncthreads();
+    const int first = threadIdx.x / lanes * (lanes / 64);
+    for (int w = 0; w < lanes / 64; ++w) most = max(most, most_of[first + w]);
+  }
+  if (!live) return;
   // 448 is 1.75 * 2^8
   const int need = min(max((int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u), 10), 246), byte = max(held, need);
   if (slot0 && byte > held) {
     // what the block held, rounded to the larger scale; factors below 2^-100 leave zeros as that does
     const float factor = __uint_as_float((uint32_t)(127 - min(byte - held, 100)) << 23);
-    for (int t = 0; t < slot0; ++t) {
+    for (int t = mine; t < slot0; t += spread) {
       u32x2* row = (u32x2*)(block + t * kD + 8 * lane.n);
       const u32x2 w = *row;
       u32x2 y;
@@ -133,34 +141,34 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
       *row = y;
     }
   }
-  if (lane.n == 0 && (!slot0 || byte != held)) *scale_at = (uint8_t)byte;
+  if (mine == 0 && lane.n == 0 && (!slot0 || byte != held)) *scale_at = (uint8_t)byte;
   const float inverse = __uint_as_float((uint32_t)(254 - byte) << 23);
   const int p0 = choose(is_v, lane.v0, lane.p0), p1 = choose(is_v, lane.v1, lane.p1);
-  for (int from = 0; from < count; from += kHeld) {
-    if (count > kHeld) ask(from);
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i) {
-      if (from + i >= count) break;
-      float y[8];
+  for (int i = 0; i < kHeld; ++i) {
+    const int t = mine + i * spread;
+    if (t >= count) break;
+    float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = to_range(x[i][e] * inverse);
-      char* row = block + (slot0 + from + i) * kD;
-      __builtin_nontemporal_store(pack_e4m3(y[0], y[1], y[2], y[3]), (int*)(row + p0));
-      __builtin_nontemporal_store(pack_e4m3(y[4], y[5], y[6], y[7]), (int*)(row + p1));
-    }
+    for (int e = 0; e < 8; ++e) y[e] = to_range(x[i][e] * inverse);
+    char* row = block + (slot0 + t) * kD;
+    __builtin_nontemporal_store(pack_e4m3(y[0], y[1], y[2], y[3]), (int*)(row + p0));
+    __builtin_nontemporal_store(pack_e4m3(y[4], y[5], y[6], y[7]), (int*)(row + p1));
   }
 }
 
 template <int kD>
 hipError_t launch_dim(const RopeLaunch& a, const Scales& scales, bool queries, hipStream_t stream) {
   constexpr int kLanes = kD / 8;
-  const int kinds = 2 * a.Hkv;
-  int threads = kinds * kLanes < kThreads ? (kinds * kLanes + 63) / 64 * 64 : kThreads;
-  const int groups = threads / kLanes, parts = (kinds + groups - 1) / groups, q_parts = (a.Hq + groups - 1) / groups;
+  // a step has one row of a block, a prompt all of them
+  const int spread = a.token_starts ? (1 << a.log_block) / kHeld : 1, lanes = kLanes * spread;
+  const int all_lanes = 2 * a.Hkv * lanes, threads = all_lanes < kThreads ? (all_lanes + 63) / 64 * 64 : kThreads;
+  const int kinds = threads / lanes, parts = (2 * a.Hkv + kinds - 1) / kinds;
+  const int rows = threads / kLanes, q_parts = (a.Hq + rows - 1) / rows;
   const int slots = a.token_starts ? (a.T >> a.log_block) + 2 * a.S : a.S;
   const int64_t append_groups = (int64_t)slots * parts, all = append_groups + (queries ? (int64_t)a.T * q_parts : 0);
   if (all * threads > UINT32_MAX) return hipErrorInvalidValue;   // a launch has fewer lanes
-  hipLaunchKernelGGL((kv_append_blk_kernel<kD>), dim3((unsigned)all), dim3(threads), 0, stream, a, scales, parts, (int)append_groups, q_parts);
+  hipLaunchKernelGGL((kv_append_blk_kernel<kD>), dim3((unsigned)all), dim3(threads), 0, stream, a, scales, spread, parts, (int)append_groups, q_parts);
   return hipGetLastError();
 }
 
