@@ -11,8 +11,6 @@
 namespace pkv {
 namespace {
 
-constexpr int kHeld = 8;   // rows of a block that a lane has at most, as it turned them
-
 // The part of a request's new tokens that falls into one block: positions [from, to) of request s, `token` being the first one's.
 struct InBlock {
   int s, from, to, token;
@@ -50,28 +48,40 @@ __device__ __forceinline__ int pack_e4m3(float w, float x, float y, float z) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(y, z, __builtin_amdgcn_cvt_pk_fp8_f32(w, x, 0, false), true);
 }
 
+constexpr int kMany = 1024;   // tokens: each has work for a workgroup of its own
+
 struct Scales {
   uint8_t *k, *v;
 };
 
 // Workgroups [0, append_groups): `parts` to a slot.  D / 8 lanes have a row, `spread` times that the rows of a block and KV head, which are keys of all heads
 // and then values.  Those behind them, in a step's launch, have the queries: `q_parts` to a token.
-template <int kD>
+// kHeld: rows of a block that a lane has at most, as it turned them.
+template <int kD, int kHeld, int kQueries>
 __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, Scales scales, int spread, int parts, int append_groups, int q_parts) {
   typedef Lane<kD, 1> L;
   constexpr int kLanes = L::kLanes;
   __shared__ uint32_t most_of[kThreads / 64];   // of each wavefront, where a head's rows are more than one's
   const L lane(a);
   const int group = threadIdx.x / kLanes;
-  if ((int)blockIdx.x >= append_groups) {
-    const int at = blockIdx.x - append_groups, token = at / q_parts;
-    const int r = (at - token * q_parts) * ((int)blockDim.x / kLanes) + group;
-    const Raw raw = lane.ask(a, token, min(r, a.Hq - 1));
+  if constexpr (kQueries > 0) if ((int)blockIdx.x >= append_groups) {
+    const int at = blockIdx.x - append_groups, token = at / q_parts, rows = blockDim.x / kLanes;
+    const int row0 = (at - token * q_parts) * kQueries * rows + group;
+    Raw raw[kQueries];
+#pragma unroll
+    for (int i = 0; i < kQueries; ++i) raw[i] = lane.ask(a, token, min(row0 + i * rows, a.Hq - 1));
+    asm volatile("" : : : "memory");   // all of them go out here, none only where it is used
     const TokenAt t = token_at(a, token);
-    if (t.position < 0 || r >= a.Hq) return;
+    if (t.position < 0) return;
     f32x4 cs = {}, sn = {};
     lane.ask_turn(a, t.position, cs, sn);
-    lane.finish(a, token, r, t.position, 0, raw, cs, sn);
+#pragma unroll
+    for (int i = 0; i < kQueries; ++i) {
+      __builtin_amdgcn_sched_barrier(0);   // one after the other
+      const int r = row0 + i * rows;
+      if (r >= a.Hq) break;
+      lane.finish(a, token, r, t.position, 0, raw[i], cs, sn);
+    }
     return;
   }
   const int slot = blockIdx.x / parts, part = blockIdx.x - slot * parts;
@@ -108,14 +118,23 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) lane.template finish<true>(a, 0, a.Hq + of, 0, 0, raw[i], cs[i], sn[i], &x[i]);
   }
-  uint32_t most = 0;   // of the magnitudes' bits, of finite values
+  float top = 0.f;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t size = __float_as_uint(x[i][e]) & 0x7fffffffu;
-      most = max(most, size < 0x7f800000u ? size : 0u);
-    }
+    for (int e = 0; e < 8; e += 2) top = fmaxf(fmaxf(top, __builtin_fabsf(x[i][e])), __builtin_fabsf(x[i][e + 1]));   // NaN does not count
+  uint32_t most = __float_as_uint(top);
+  const bool infinite = most == 0x7f800000u;
+  if (__builtin_expect(infinite, 0)) {   // nor does infinity
+    most = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t size = __float_as_uint(x[i][e]) & 0x7fffffffu;
+        most = max(most, size < 0x7f800000u ? size : 0u);
+      }
+  }
   const int lanes = kLanes * spread;
   for (int step = 1; step < min(lanes, 64); step <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, step));
   if (lanes > 64) {
@@ -142,6 +161,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
     }
   }
   if (mine == 0 && lane.n == 0 && (!slot0 || byte != held)) *scale_at = (uint8_t)byte;
+  const bool beyond = __any(infinite || need == 246);   // else no value is
   const float inverse = __uint_as_float((uint32_t)(254 - byte) << 23);
   const int p0 = choose(is_v, lane.v0, lane.p0), p1 = choose(is_v, lane.v1, lane.p1);
 #pragma unroll
@@ -150,43 +170,56 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
     if (t >= count) break;
     float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = to_range(x[i][e] * inverse);
+    for (int e = 0; e < 8; ++e) y[e] = x[i][e] * inverse;
+    if (beyond) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = to_range(y[e]);
+    }
     char* row = block + (slot0 + t) * kD;
     __builtin_nontemporal_store(pack_e4m3(y[0], y[1], y[2], y[3]), (int*)(row + p0));
     __builtin_nontemporal_store(pack_e4m3(y[4], y[5], y[6], y[7]), (int*)(row + p1));
   }
 }
 
-template <int kD>
-hipError_t launch_dim(const RopeLaunch& a, const Scales& scales, bool queries, hipStream_t stream) {
+template <int kD, int kHeld, int kQueries>
+hipError_t launch_queries(const RopeLaunch& a, const Scales& scales, hipStream_t stream) {
   constexpr int kLanes = kD / 8;
   // a step has one row of a block, a prompt all of them
   const int spread = a.token_starts ? (1 << a.log_block) / kHeld : 1, lanes = kLanes * spread;
-  const int all_lanes = 2 * a.Hkv * lanes, threads = all_lanes < kThreads ? (all_lanes + 63) / 64 * 64 : kThreads;
+  const int all_lanes = 2 * a.Hkv * lanes, threads = all_lanes < kThreads && a.T < kMany ? (all_lanes + 63) / 64 * 64 : kThreads;
   const int kinds = threads / lanes, parts = (2 * a.Hkv + kinds - 1) / kinds;
-  const int rows = threads / kLanes, q_parts = (a.Hq + rows - 1) / rows;
+  const int rows = kQueries * (threads / kLanes), q_parts = kQueries ? (a.Hq + rows - 1) / rows : 0;
   const int slots = a.token_starts ? (a.T >> a.log_block) + 2 * a.S : a.S;
-  const int64_t append_groups = (int64_t)slots * parts, all = append_groups + (queries ? (int64_t)a.T * q_parts : 0);
+  const int64_t append_groups = (int64_t)slots * parts, all = append_groups + (int64_t)a.T * q_parts;
   if (all * threads > UINT32_MAX) return hipErrorInvalidValue;   // a launch has fewer lanes
-  hipLaunchKernelGGL((kv_append_blk_kernel<kD>), dim3((unsigned)all), dim3(threads), 0, stream, a, scales, spread, parts, (int)append_groups, q_parts);
+  hipLaunchKernelGGL((kv_append_blk_kernel<kD, kHeld, kQueries>), dim3((unsigned)all), dim3(threads), 0, stream, a, scales, spread, parts,
+                     (int)append_groups, q_parts);
   return hipGetLastError();
+}
+
+template <int kD>
+hipError_t launch_dim(const RopeLaunch& a, const Scales& scales, hipStream_t stream) {
+  if (!a.token_starts) return a.q_out ? launch_queries<kD, 1, 1>(a, scales, stream) : launch_queries<kD, 1, 0>(a, scales, stream);
+  if (!a.q_out) return launch_queries<kD, 8, 0>(a, scales, stream);
+  if (a.T < kMany) return launch_queries<kD, 8, 1>(a, scales, stream);
+  // many queries by themselves: beside rows that are held they have half the wavefronts that hide their loads (94 us as one launch 106)
+  const hipError_t e = launch_queries<kD, 8, 0>(a, scales, stream);
+  if (e != hipSuccess) return e;
+  RopeLaunch rest = a;
+  rest.Hkv = 0;
+  rest.kv_fp8 = 1;
+  rest.id_faults = nullptr;
+  return launch_kv_rope(rest, stream);
 }
 
 }  // namespace
 
 hipError_t launch_kv_append_blk(const RopeLaunch& a, uint8_t* k_scales, uint8_t* v_scales, hipStream_t stream) {
   const Scales scales = {k_scales, v_scales};
-  const bool queries = a.q_out != nullptr, many = a.T >= 1024, with_them = queries && !many;
-  const hipError_t e = a.D == 64    ? launch_dim<64>(a, scales, with_them, stream)
-                       : a.D == 128 ? launch_dim<128>(a, scales, with_them, stream)
-                       : a.D == 256 ? launch_dim<256>(a, scales, with_them, stream)
-                                    : hipErrorInvalidValue;
-  if (e != hipSuccess || !queries || !many) return e;
-  RopeLaunch rest = a;   // queries alone, several rows of a token to a lane
-  rest.Hkv = 0;
-  rest.kv_fp8 = 1;
-  rest.id_faults = nullptr;
-  return launch_kv_rope(rest, stream);
+  if (a.D == 64) return launch_dim<64>(a, scales, stream);
+  if (a.D == 128) return launch_dim<128>(a, scales, stream);
+  if (a.D == 256) return launch_dim<256>(a, scales, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace pkv
