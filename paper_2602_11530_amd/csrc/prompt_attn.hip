@@ -43,12 +43,13 @@ struct Tokens {
 };
 // Slots of `per` tokens: request s has slots start / per + s and on, one or none of them empty.
 __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int per) {
-  int s, from, end;
+  int s, from, end, L;
   if (!a.token_starts) {
     s = from = slot;
     end = from + 1;
     if (s >= a.S) return {0, 0, 0, 0};
     slot = 0;
+    L = *(ScalarLoad)(a.context_lens + s);
   } else {
     // the last request whose slots begin at or before this one: one look of 64 lanes up to 63 requests, else two, kMaxSeqs being 32 times 64
     const int lane = threadIdx.x & 63, step = (a.S >> 6) + 1;
@@ -59,14 +60,16 @@ __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int
       base = max(__popcll(__ballot(i < a.S && start(i) / per + i <= slot)) - 1, 0) * step;
     }
     const int j = base + lane, at = start(j);
+    const int length = j < a.S ? a.context_lens[j] : 0;          // with the starts: one round trip less
     const int found = __popcll(__ballot(j < a.S && lane < 63 && at / per + j <= slot)) - 1;
     if (found < 0) return {0, 0, 0, 0};
     s = base + found;
     from = __builtin_amdgcn_readlane(at, found);
     end = __builtin_amdgcn_readlane(at, found + 1);
     slot -= from / per + s;
+    L = __builtin_amdgcn_readlane(length, found);
   }
-  const int L = min(max(*(ScalarLoad)(a.context_lens + s), 0), a.max_ctx);
+  L = min(max(L, 0), a.max_ctx);
   const int n = end - from;
   // tokens before position 0 have none
   const int skip = max(n - L, 0);
@@ -504,11 +507,11 @@ PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
   // Few workgroups over long contexts: those are cut.  Into as many pieces as give the least time by this estimate, in us: workgroups in turns of as many
   // as run at once, a tile 2 us (D = 128), a start 3 tiles, and the pieces' rows written and read.
   const int64_t tiles = ((int64_t)max_ctx + prompt_keys(D) - 1) / prompt_keys(D), groups = p.slots * Hkv, at_once = 256 * prompt_groups(D);
-  const double tile_us = 2.0 * D / 128, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
+  const double tile_us = 2.0 * D / 128 * prompt_keys(D) / 64, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
   p.piece = (int)(tiles > 0 ? tiles : 1);
   p.pieces = 1;
   double least = 0;
-  for (int64_t n = 1; n <= kMaxPieces && 4 * n <= tiles + 3; ++n) {
+  for (int64_t n = 1; n <= kMaxPieces && 4 * n <= tiles + 3 && (n == 1 || (groups < 2 * at_once && groups * n <= 8 * at_once)); ++n) {
     const int64_t piece = (tiles + n - 1) / n;
     const double us = (double)((groups * n + at_once - 1) / at_once) * (piece + 3) * tile_us + (n > 1 ? 5 + n * join_us : 0);
     if (n == 1 || us < least) {
@@ -516,7 +519,6 @@ PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
       p.piece = (int)piece;
       p.pieces = (int)((tiles + piece - 1) / piece);
     }
-    if (groups * n > 8 * at_once) break;
   }
   return p;
 }
