@@ -26,6 +26,7 @@ typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
 
 constexpr float kLazyLog2 = 8.f;
 constexpr float kLeast = -3e38f;                  // a reference maximum before any score: finite, so that what is masked, -inf, gives weights of zero
+constexpr float kTooLarge = 0x1p120f;              // a scale whose products with e4m3 values may not be finite
 constexpr int kRawBuffer = 0x00020000;
 constexpr int kMfma = 0x8, kDsRead = 0x100;       // kinds of instructions, for the scheduler
 constexpr int kReadsAhead = 6;
@@ -110,8 +111,10 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   constexpr int kTileBytes = kKeyTile * kD * 2;
   constexpr int kElem = kFormat == 0 ? 2 : 1;
   constexpr int kSource = kKeyTile * kD * kElem / 16;            // 16-byte pieces of a tile as the pool has it
-  constexpr int kLoads = (kSource + kThreads - 1) / kThreads;    // of a lane
+  constexpr int kLoads = kSource / kThreads;                     // of a lane
   constexpr int kPerToken = kD * kElem / 16;
+  constexpr int kOfUnit = kPerToken * kBlockTokens;
+  static_assert(kLoads * kThreads == kSource && kOfUnit % (64 * kLoads) == 0, "a wavefront loads pieces of one unit");
   constexpr bool kDirect = kFormat == 0;                         // nothing to widen: from memory straight into LDS
   __shared__ __align__(16) char lds[4 * kTileBytes];             // K and V of two tiles in turn
   __shared__ int first_bad[kD];                                  // the first key whose V is not finite there, of those that some row does not see
@@ -184,18 +187,19 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   int window_at = from / kWindowTiles * kWindowTiles;
   Window now = describe(window_at), then = describe(window_at + kWindowTiles);
 
+  auto piece_of = [&](int i) { return (wave * kLoads + i) * 64 + lane; };   // of a tile
   // kDirect: the memory unit writes 64 pieces in a row to LDS, so that each lane asks for the piece whose place is its own.
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   int k_from[kLoads], v_from[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    const int at = (i * kThreads + threadIdx.x) % (kPerToken * kBlockTokens), t = at / kPerToken, here = at % kPerToken;
+    const int at = piece_of(i) % kOfUnit, t = at / kPerToken, here = at % kPerToken;
     k_from[i] = t * (kD * kElem) + k_place<kD>(t, here) % (kD * 2);
     v_from[i] = t * (kD * kElem) + v_place<kD>(t, here) % (kD * 2);
   }
   // A tile on its way: out of memory into registers, from there into LDS.
   u32x4 kr[kLoads], vr[kLoads];
-  float ks[kLoads], vs[kLoads];
+  float ks = 1.f, vs = 1.f;
   uint32_t unmapped = 0;      // of the tile that was asked for last, a bit for each unit that is not there
   auto ask = [&](int tile, int at_place) {
     if (tile >= window_at + kWindowTiles) {
@@ -205,31 +209,27 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     }
     const int u0 = kUnits * (tile - window_at);
     unmapped = (uint32_t)(now.gone >> u0) & ((1 << kUnits) - 1);
+    const int u = u0 + wave * kLoads * 64 / kOfUnit;
+    const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(now.at >> 32), u) << 32 |
+                        (uint32_t)__builtin_amdgcn_readlane((int)now.at, u);
+    const int bytes = __builtin_amdgcn_readlane(now.bytes, u);
+    const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, kRawBuffer);
+    const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)(at + v_behind), 0, bytes, kRawBuffer);
+    if constexpr (kFormat == kBlkPools) {
+      const int both = __builtin_amdgcn_readlane(now.scales, u);
+      ks = __uint_as_float((uint32_t)(both & 0xff) << 23);
+      vs = __uint_as_float((uint32_t)(both >> 8) << 23);
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int piece = i * kThreads + wave * 64;                // the wavefront's first
-      const int u = u0 + piece / kPerToken / kBlockTokens;
-      if (kSource % kThreads != 0 && piece >= kSource) break;
-      const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(now.at >> 32), u) << 32 |
-                          (uint32_t)__builtin_amdgcn_readlane((int)now.at, u);
-      const int bytes = __builtin_amdgcn_readlane(now.bytes, u);
-      const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, kRawBuffer);
-      const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)(at + v_behind), 0, bytes, kRawBuffer);
       if constexpr (kDirect) {
-        const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * piece;
+        const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * 64 * (wave * kLoads + i);
         load_to_lds(kb, to_lds, k_from[i]);
         load_to_lds(vb, to_lds + kTileBytes, v_from[i]);
-        continue;
-      }
-      const int offset = 16 * ((piece + lane) % (kPerToken * kBlockTokens));
-      kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, 0));
-      vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, 0));
-      if constexpr (kFormat == kBlkPools) {
-        const int both = __builtin_amdgcn_readlane(now.scales, u);
-        ks[i] = __uint_as_float((uint32_t)(both & 0xff) << 23);
-        vs[i] = __uint_as_float((uint32_t)(both >> 8) << 23);
       } else {
-        ks[i] = vs[i] = 1.f;
+        const int offset = 16 * (piece_of(i) % kOfUnit);
+        kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, 0));
+        vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, 0));
       }
     }
   };
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
       if constexpr (kFormat == 0) bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
       else bad |= (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
     }
-    const bool all = kFormat == kBlkPools && !(vs[i] < 0x1p120f);
+    const bool all = kFormat == kBlkPools && !(vs < kTooLarge);
     if (!bad && !all) return;
     any_bad = 1;
 #pragma unroll
@@ -256,7 +256,6 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
         vr[i][e * kElem / 4] &= ~((kFormat == 0 ? 0xffffu : 0xffu) << shift);
       }
     }
-    if (all) vs[i] = 1.f;
   };
   // kDirect: what has arrived is in place; of a tile that is looked at this lane's pieces of V are read back.
   auto arrived = [&](int tile, char* v_lds, bool look) {
@@ -264,8 +263,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     if (!look) return;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int piece = i * kThreads + threadIdx.x;
-      if (kSource % kThreads != 0 && piece >= kSource) break;
+      const int piece = piece_of(i);
       u32x4* at = (u32x4*)(v_lds + 16 * piece);
       vr[i] = *at;
       const u32x4 was = vr[i];
@@ -274,10 +272,10 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     }
   };
   auto put = [&](int tile, char* k_lds, char* v_lds, bool look) {
+    const float v_by = look && !(vs < kTooLarge) ? 1.f : vs;     // held back, all of it
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int piece = i * kThreads + threadIdx.x;
-      if (kSource % kThreads != 0 && piece >= kSource) break;
+      const int piece = piece_of(i);
       const int t = piece / kPerToken, p = piece % kPerToken;
       if (look) hold_back(i, tile, t, p);
       if constexpr (kFormat == 0) {
@@ -286,9 +284,9 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
       } else {
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const u32x2 k0 = widen(kr[i][2 * z], ks[i]), k1 = widen(kr[i][2 * z + 1], ks[i]);
+          const u32x2 k0 = widen(kr[i][2 * z], ks), k1 = widen(kr[i][2 * z + 1], ks);
           *(u32x4*)(k_lds + k_place<kD>(t, 2 * p + z)) = u32x4{k0.x, k0.y, k1.x, k1.y};
-          const u32x2 v0 = widen(vr[i][2 * z], vs[i]), v1 = widen(vr[i][2 * z + 1], vs[i]);
+          const u32x2 v0 = widen(vr[i][2 * z], v_by), v1 = widen(vr[i][2 * z + 1], v_by);
           *(u32x4*)(v_lds + v_place<kD>(t, 2 * p + z)) = u32x4{v0.x, v0.y, v1.x, v1.y};
         }
       }
