@@ -555,7 +555,7 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
  * bf16 inputs, fp32 scores, softmax statistics and accumulation; a weight is rounded to bf16
  * before it multiplies V (relative error 2^-8), and a row once, to bf16, at the end.  No bit of a row depends on where
  * its blocks are nor on the other requests' contents, but its last bits depend on T, num_seqs and
- * max_context_len, which choose how contexts are cut, and on token_starts[s] modulo the tokens of a workgroup's rows.
+ * max_context_len, which choose how contexts are cut.
  *
  *   q             device  bf16  [T][Hq][D], rows of tokens without gaps
  *   token_starts  device  int32 [num_seqs + 1], ascending, or NULL: one token for each request, T = num_seqs

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
   const int slot0 = at.from & ((1 << a.log_block) - 1);   // rows before it were there
   uint8_t* scale_at = (is_v ? scales.v : scales.k) + (int64_t)id * scale_row_bytes(a.Hkv) + head;
   char* block = (char*)(is_v ? a.v_pool : a.k_pool) + (((int64_t)id * a.Hkv + head) << a.log_block) * kD;
-  const int held = slot0 ? min(max((int)*scale_at, 10), 246) : 0;
+  const int held = slot0 ? *scale_at : 0;
 
   // this lane's rows: `mine`, `mine` + spread and on, at most kHeld of them
   float x[kHeld][8];
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_blk_kernel(RopeLaunch a, S
   }
   if (mine == 0 && lane.n == 0 && (!slot0 || byte != held)) *scale_at = (uint8_t)byte;
   const bool beyond = __any(infinite || need == 246);   // else no value is
-  const float inverse = __uint_as_float((uint32_t)(254 - byte) << 23);
+  const float inverse = __builtin_ldexpf(1.f, 127 - byte);   // a subnormal number for a byte of 254, which was there
   const int p0 = choose(is_v, lane.v0, lane.p0), p1 = choose(is_v, lane.v1, lane.p1);
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {

@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   const int head = row - which * a.G;
   const bool live = which < tok.count;
   which = min(which, tok.count - 1);
-  const int64_t q_row = ((int64_t)(tok.first + which) * a.Hq + kvh * a.G + head) * kD;
+  const int of_call = (tok.first + which) * a.Hq + kvh * a.G + head;   // T * Hq is below 2^31
   const int last_key = tok.at + which;
   const int wave_from = __builtin_amdgcn_readlane(last_key, 0), wave_to = __builtin_amdgcn_readlane(last_key, 31);
   const bool idle = __builtin_amdgcn_readfirstlane(!__any(live));
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   const float scale = fmaxf(__builtin_fabsf(a.scale_log2e), 0x1p-126f);   // masked scores stay -inf with a scale of zero, too
 #pragma unroll
   for (int jj = 0; jj < kSteps; ++jj) {
-    u32x4 x = *(const u32x4*)(a.q + q_row + 16 * jj + 8 * h);
+    u32x4 x = *(const u32x4*)(a.q + (int64_t)of_call * kD + 16 * jj + 8 * h);
     if (negative) x ^= 0x80008000u;
     q[jj] = __builtin_bit_cast(bf16x8, x);
   }
@@ -155,7 +155,6 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   // at a time, and read from the lane.
   struct Window {
     uint64_t at;    // of the unit's K, 16 keys of the KV head
-    int bytes;      // of its rows that are there
     int scales;     // kBlkPools: of K, of V
     uint64_t gone;  // a bit for each unit that is not there
   };
@@ -173,7 +172,6 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     Window w;
     const int slab = mapped ? ((id * a.Hkv + kvh) << log_units) + (u & ((1 << log_units) - 1)) : 0;
     w.at = (uint64_t)a.k_pool + (uint64_t)slab * (kBlockTokens * kD * kElem);
-    w.bytes = mapped ? min(kBlockTokens, context - u * kBlockTokens) * (kD * kElem) : 0;
     w.gone = __ballot(!mapped);
     w.scales = 0;
     if constexpr (kFormat == kBlkPools) {
@@ -212,7 +210,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     const int u = u0 + wave * kLoads * 64 / kOfUnit;
     const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(now.at >> 32), u) << 32 |
                         (uint32_t)__builtin_amdgcn_readlane((int)now.at, u);
-    const int bytes = __builtin_amdgcn_readlane(now.bytes, u);
+    const int rows = now.gone >> u & 1 ? 0 : min(kBlockTokens, context - (kUnits * window_at + u) * kBlockTokens), bytes = rows * (kD * kElem);
     const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, kRawBuffer);
     const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)(at + v_behind), 0, bytes, kRawBuffer);
     if constexpr (kFormat == kBlkPools) {
@@ -414,6 +412,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
         if (first_bad[32 * d + 8 * (r >> 2) + 4 * h + (r & 3)] <= last_key) o[d][r] = __builtin_nanf("");
   }
   const float total = l + __shfl_xor(l, 32);
+  const int64_t q_row = (int64_t)of_call * kD;
   if (tiles <= a.piece) {
     const float inv = inverse(total, a.out_scale);
 #pragma unroll
@@ -429,7 +428,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(f32x4*)(part + 32 * d + 8 * g + 4 * h) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
-    if (h == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + q_row / kD) * 2) = f32x2{m == kLeast ? kNegInf : m, total};
+    if (h == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + of_call) * 2) = f32x2{m == kLeast ? kNegInf : m, total};
   }
 }
 

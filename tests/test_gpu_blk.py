@@ -295,3 +295,80 @@ def test_captured_and_on_another_stream():
         torch.cuda.synchronize()
         plain.within(to_bits(out), *want)
     compare_pools(p, b)
+
+
+@pytest.mark.parametrize("dim,block", [(128, 16), (64, 64)])
+def test_appends_behind_scales_of_any_byte(dim, block):
+    """Blocks that were not filled by appends may hold scales that those would not choose: they are kept, or grow, as any other."""
+    bytes_ = [0, 1, 9, 10, 11, 120, 127, 245, 246, 247, 253, 254, 255]
+    b = make_batch([5] * len(bytes_), [3] * len(bytes_), 2, 1, dim, block, 9)
+    p = pools_of(b, "blk")
+    for s, byte in enumerate(bytes_):
+        p.k_scales[b.tables[s][0], 0] = byte
+        p.v_scales[b.tables[s][0], 0] = bytes_[-1 - s]
+    refresh(p, b)
+    upload(p)
+    (k, v), values = new_rows(b, b.tokens)
+    pkv.kv_rope_append_fp8blk(None, to_dev(k), to_dev(v), None, None, None, None, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, to_dev(b.tables), to_dev(b.lens),
+                              to_dev(b.starts), pkv.make_rope(b.tokens, 0, 0), shape_of(b))
+    torch.cuda.synchronize()
+    plain_append(p, b, values, plain.positions(b.lens, b.starts, 1 << 30, b.tokens))
+    for name in "kv":   # what a block of NaN holds is nothing
+        nan = getattr(p, name + "_scales")[:, 0] == 255
+        getattr(p, name + "_bits")[nan] = getattr(p, name + "_dev").cpu().numpy()[nan]
+    compare_pools(p, b)
+
+
+def test_beyond_4_gib():
+    """150 000 blocks of 32 KiB, the requests' own on both sides of 4 GiB and at the end: appends, attention of prompts and of steps."""
+    if torch.cuda.mem_get_info()[0] < 14 << 30:
+        pytest.skip("needs 14 GiB of free device memory")
+    from prompt_util import check, plain_prompt, run_prompt
+    large, hkv, dim = 150_000, 8, 256
+    b = make_batch([0, 170, 1000], [37, 30, 1], 16, hkv, dim, 16, 10)
+    nbytes = hkv * 16 * dim
+    assert large * nbytes > 1 << 32
+    small = pools_of(b, "blk")
+    place = np.concatenate([[large - 1, (1 << 32) // nbytes, (1 << 32) // nbytes + 1],
+                            b.rng.choice(np.arange((1 << 32) // nbytes + 2, large - 1), b.num_blocks - 3, replace=False)])
+    p = pools_of(b, "blk")
+    p.k_dev, p.v_dev = (torch.zeros((large, hkv, 16, dim), dtype=torch.uint8, device="cuda") for _ in range(2))
+    p.ks_dev, p.vs_dev = (torch.zeros((large, scale_row(hkv)), dtype=torch.uint8, device="cuda") for _ in range(2))
+    at = to_dev(place.astype(np.int64))
+    tables, count = b.tables, b.num_blocks
+    far = np.where(tables >= 0, place[tables], -1).astype(np.int32)
+    (k, v), values = new_rows(b, b.tokens, 1.0)
+    for name in "kv":
+        getattr(p, name + "_dev")[at] = to_dev(getattr(small, name + "_bits"))
+        getattr(p, name[0] + "s_dev")[at] = to_dev(getattr(small, name + "_scales"))
+    b.tables, b.num_blocks = far, large
+    pkv.kv_rope_append_fp8blk(None, to_dev(k), to_dev(v), None, None, None, None, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, to_dev(far), to_dev(b.lens),
+                              to_dev(b.starts), pkv.make_rope(b.tokens, 0, 0), shape_of(b))
+    got = run_prompt(b, p)
+    q = b.q_bits
+    b.q_bits = q[:3].copy()
+    step = step_attention(b, p)
+    b.q_bits, b.tables, b.num_blocks = q, tables, count
+    plain_append(small, b, values, plain.positions(b.lens, b.starts, 1 << 30, b.tokens))
+    for name in "kv":
+        assert np.array_equal(getattr(p, name + "_dev")[at].cpu().numpy(), getattr(small, name + "_bits"))
+        assert np.array_equal(getattr(p, name[0] + "s_dev")[at].cpu().numpy(), getattr(small, name + "_scales"))
+    check(b, got, *plain_prompt(b, small))
+    b.q_bits = q[:3].copy()
+    plain.within(step, *plain.attention(values_of(b), small.k, small.v, tables, b.lens, b.scale))
+
+
+@pytest.mark.parametrize("hkv", [17, 40])
+def test_more_kv_heads_than_one_row_of_scales(hkv):
+    b = make_batch([30, 0, 1], [20, 50, 1], hkv, hkv, 64, 32, hkv)
+    p = pools_of(b, "blk")
+    (k, v), values = new_rows(b, b.tokens, 1.0)
+    pkv.kv_rope_append_fp8blk(None, to_dev(k), to_dev(v), None, None, None, None, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, to_dev(b.tables), to_dev(b.lens),
+                              to_dev(b.starts), pkv.make_rope(b.tokens, 0, 0), shape_of(b))
+    from prompt_util import check, plain_prompt, run_prompt
+    got = run_prompt(b, p)
+    plain_append(p, b, values, plain.positions(b.lens, b.starts, 1 << 30, b.tokens))
+    compare_pools(p, b)
+    check(b, got, *plain_prompt(b, p))
+    b.q_bits = b.q_bits[:3]
+    plain.within(step_attention(b, p), *plain.attention(values_of(b), p.k, p.v, b.tables, b.lens, b.scale))

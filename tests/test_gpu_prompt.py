@@ -3,9 +3,11 @@ import numpy as np
 import pytest
 import torch
 
+import plain
+from gpu_util import to_bits, to_dev
 from paper_2602_11530_amd import binding as pkv
 from paper_2602_11530_amd import workloads as wl
-from prompt_util import KINDS, check, make_batch, plain_prompt, pools_of, run_prompt, shape_of, upload
+from prompt_util import KINDS, check, make_batch, plain_append, plain_prompt, pools_of, refresh, run_prompt, shape_of, upload
 
 pytestmark = pytest.mark.gpu
 
@@ -207,3 +209,139 @@ def test_on_another_stream_and_captured():
         torch.cuda.synchronize()
         for o in outs:
             assert np.array_equal(o.cpu().numpy().view(np.uint16), want)
+
+
+def test_scales_that_are_not_finite():
+    """Of V's blocks with a scale of NaN, or one whose products are infinite, only the rows that see a token of them have anything."""
+    b = make_batch([20, 0], [70, 90], 4, 2, 128, 16, 16)
+    p = pools_of(b, "blk")
+    p.v_scales[b.tables[0][4], 1], p.v_scales[b.tables[1][1], 0] = 255, 254       # tokens 64 to 79 and 16 to 31
+    p.v_bits[b.tables[1][1], 0] = 0x7E                                            # 448
+    upload(p)
+    got = wl.bf16_bits_to_f64(run_prompt(b, p)).reshape(b.q_bits.shape)
+    at = b.lens.repeat(b.new) - np.repeat(b.starts[1:], b.new) + np.arange(b.tokens)
+    bad = np.zeros(got.shape, bool)
+    bad[(np.arange(b.tokens) < 70) & (at >= 64), 2:] = True
+    bad[(np.arange(b.tokens) >= 70) & (at >= 16), :2] = True
+    assert np.isfinite(got[~bad]).all() and not np.isfinite(got[bad]).any()
+    refresh(p, b)
+    with np.errstate(all="ignore"):
+        want, off, has = plain_prompt(b, p)
+    check(b, run_prompt(b, p), np.where(bad, np.nan, want), np.where(bad, np.inf, off), has)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_long_tables(kind):
+    """Contexts of many windows of the table, most entries behind them empty, a bound far above the lengths."""
+    b = make_batch([5000, 9000, 0, 2047], [3, 33, 2, 1], 4, 1, 64, 16, 17)
+    b.tables = np.concatenate([b.tables, np.full((4, 3000), -1, np.int32)], axis=1)
+    b.tables[:, -1] = 2 ** 31 - 1
+    p = pools_of(b, kind)
+    check(b, run_prompt(b, p), *plain_prompt(b, p))
+
+
+def test_two_calls_at_once():
+    """On two streams, with a workspace each, over the same pools."""
+    a = make_batch([3000, 5], [4, 60], 8, 2, 128, 16, 18)
+    p = pools_of(a, "fp8")
+    assert pkv.pkv_prompt_workspace_bytes(shape_of(a), a.tokens) > 0
+    want = run_prompt(a, p)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = [run_prompt(a, p, stream=s, wait=False) for s in streams]
+        torch.cuda.synchronize()
+        assert all(np.array_equal(want, to_bits(x)) for x in got)
+
+
+def test_rows_beyond_4_gib():
+    """A call whose queries are 4.6 GiB: the last requests' rows are right, and the first one's."""
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GiB of free device memory")
+    heads, dim, seqs, new = 64, 256, 1100, 135
+    b = make_batch([0] * 3, [new] * 3, heads, 8, dim, 64, 19)
+    p = pools_of(b, "bf16")
+    # the three requests again and again, over the same blocks
+    tables, starts = np.tile(b.tables, (seqs // 3 + 1, 1))[:seqs], (np.arange(seqs + 1) * new).astype(np.int32)
+    lens, tokens = np.full(seqs, new, np.int32), seqs * new
+    assert tokens * heads * dim * 2 > 1 << 32
+    few = to_dev(b.q_bits)
+    q = few.repeat(seqs // 3 + 1, 1, 1)[:tokens].contiguous()
+    out = torch.full_like(q, 0x7FC1)
+    shape = pkv.make_shape(seqs, heads, 8, tables.shape[1], b.num_blocks, dim, 64, 0, 0)
+    ws = torch.empty(max(pkv.pkv_prompt_workspace_bytes(shape, tokens), 16), dtype=torch.uint8, device="cuda")
+    pkv.paged_prompt_attn(q, p.k_dev, p.v_dev, to_dev(tables), to_dev(lens), to_dev(starts), tokens, b.scale, out, shape, ws)
+    torch.cuda.synchronize()
+    first = out[:3 * new]
+    check(b, to_bits(first), *plain_prompt(b, p))
+    whole = seqs // 3 * 3 * new
+    assert torch.equal(out[:whole].view(seqs // 3, -1), first.reshape(1, -1).expand(seqs // 3, -1))
+    assert torch.equal(out[whole:], first[:tokens - whole])
+
+
+def test_one_token_after_another_as_a_program_goes():
+    """Prompts, then steps, each captured in a graph of its own; the graphs share one workspace and run in turn on one stream."""
+    b = make_batch([0, 0], [70, 33], 8, 2, 128, 16, 20, spare=20)
+    p = pools_of(b, "blk")
+    b.tables = b.rng.permutation(b.num_blocks)[:2 * 8].reshape(2, 8).astype(np.int32)
+    total = 6
+    rows = [wl.normal_bf16(b.rng, (b.tokens + 2 * total, h, 128)) for h in (8, 2, 2)]
+    q, k, v = (to_dev(x) for x in rows)
+    tables, starts, step_starts = to_dev(b.tables), to_dev(b.starts), None
+    lens = to_dev(b.lens)
+    shape = shape_of(b)
+    need = max(pkv.pkv_prompt_workspace_bytes(shape, b.tokens), pkv.pkv_attn_workspace_bytes(shape), 16)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    q_in, k_in, v_in = (torch.empty((2, h, 128), dtype=torch.int16, device="cuda") for h in (8, 2, 2))
+    turned, turned_step = torch.empty_like(q[:b.tokens]), torch.empty_like(q_in)
+    out, out_step = torch.empty_like(turned), torch.empty_like(turned_step)
+
+    def prompt():
+        pkv.kv_rope_append_fp8blk(q[:b.tokens], k[:b.tokens], v[:b.tokens], None, None, None, turned, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, tables, lens,
+                                  starts, pkv.make_rope(b.tokens, 0, 0), shape)
+        pkv.paged_prompt_attn_fp8blk(turned, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, tables, lens, starts, b.tokens, b.scale, out, shape, ws)
+
+    def step():
+        pkv.kv_rope_append_fp8blk(q_in, k_in, v_in, None, None, None, turned_step, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, tables, lens, step_starts,
+                                  pkv.make_rope(2, 0, 0), shape)
+        pkv.paged_decode_attn_fp8blk(turned_step, p.k_dev, p.v_dev, p.ks_dev, p.vs_dev, tables, lens, b.scale, out_step, shape, ws)
+
+    torch.cuda.synchronize()
+    graphs = []
+    for run in (prompt, step):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run()
+        graphs.append(graph)
+    values = [wl.bf16_bits_to_f64(x).reshape(x.shape) for x in rows[1:]]
+    first_lens, all_q = b.lens.copy(), rows[0]
+    fresh = {name: getattr(p, name).copy() for name in ("k_bits", "v_bits", "k_scales", "v_scales")}
+    for turn in range(2):      # the same program twice, over what the first left in the pools
+        b.lens = first_lens.copy()
+        lens.copy_(to_dev(b.lens))
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        plain_append(p, b, [x[:b.tokens] for x in values], plain.positions(b.lens, b.starts, 1 << 30, b.tokens))
+        b.q_bits = all_q[:b.tokens]
+        check(b, to_bits(out), *plain_prompt(b, p))
+        for i in range(total):
+            at = b.tokens + 2 * i
+            b.lens = b.lens + 1
+            for x, y in ((q_in, q), (k_in, k), (v_in, v)):
+                x.copy_(y[at:at + 2])
+            lens.add_(1)
+            graphs[1].replay()
+            torch.cuda.synchronize()
+            plain_append(p, b, [x[at:at + 2] for x in values], [(s, int(n) - 1) for s, n in enumerate(b.lens)])
+            b.q_bits = all_q[at:at + 2]
+            got = to_bits(out_step)
+            query = wl.bf16_bits_to_f64(b.q_bits).reshape(b.q_bits.shape)
+            plain.within(got, *plain.attention(query, p.k, p.v, b.tables, b.lens, b.scale))
+            # the same step as a prompt of one token each
+            b.starts, kept = np.arange(3, dtype=np.int32), (b.starts, b.tokens)
+            b.tokens = 2
+            check(b, run_prompt(b, p), *plain_prompt(b, p))
+            b.starts, b.tokens = kept
+        for name in ("k", "v"):
+            assert np.array_equal(getattr(p, name + "_dev").cpu().numpy(), getattr(p, name + "_bits"))
+            assert np.array_equal(getattr(p, name + "s_dev").cpu().numpy(), getattr(p, name + "_scales"))
+    assert any(not np.array_equal(fresh[n], getattr(p, n)) for n in fresh)
