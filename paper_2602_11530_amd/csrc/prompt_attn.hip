@@ -29,14 +29,14 @@ constexpr float kLeast = -3e38f;                  // a reference maximum before 
 constexpr float kTooLarge = 0x1p120f;              // a scale whose products with e4m3 values may not be finite
 constexpr int kRawBuffer = 0x00020000;
 constexpr int kMfma = 0x8, kDsRead = 0x100;       // kinds of instructions, for the scheduler
-constexpr int kReadsAhead = 6;
-// Keys of a tile.
-__host__ __device__ constexpr int prompt_keys(int D) { return D == 256 ? 32 : 64; }
+
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kMaxPieces = 64;                    // of a context
+// Keys of a tile, where contexts are cut and where they are whole.
+__host__ __device__ constexpr int prompt_keys(int D, bool cut) { return D == 256 || (D == 128 && !cut) ? 32 : 64; }
 // Workgroups that run on a compute unit at once, by their registers and LDS.
-constexpr int prompt_groups(int D) { return D == 64 ? 4 : D == 128 ? 2 : 1; }
+constexpr int prompt_groups(int D, int keys) { return D == 64 ? 4 : D == 128 && keys == 32 ? 3 : 2; }
 
 // A workgroup's tokens: `first` to `first + count` of the call, of request s, at position `at` and on.
 struct Tokens {
@@ -102,10 +102,10 @@ template <int kD> __device__ __forceinline__ int v_place(int t, int p) {
   return (t * kPieces + (p ^ (turn << 2))) * 16;
 }
 
-template <int kD, int kFormat>
-__global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kernel(PromptLaunch a, int per, int slots, uint32_t group_inverse) {
+template <int kD, int kFormat, int kKeyTile>
+__global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_attn_kernel(PromptLaunch a, int per, int slots, uint32_t group_inverse) {
   constexpr int kSteps = kD / 16, kTiles = kD / 32;
-  constexpr int kKeyTile = prompt_keys(kD), kHalves = kKeyTile / 32;
+  constexpr int kHalves = kKeyTile / 32;
   constexpr int kUnits = kKeyTile / kBlockTokens;                // of a tile
   constexpr int kWindowTiles = 64 / kUnits;                      // whose units a wavefront's lanes describe
   constexpr int kTileBytes = kKeyTile * kD * 2;
@@ -115,8 +115,11 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   constexpr int kPerToken = kD * kElem / 16;
   constexpr int kOfUnit = kPerToken * kBlockTokens;
   static_assert(kLoads * kThreads == kSource && kOfUnit % (64 * kLoads) == 0, "a wavefront loads pieces of one unit");
+  constexpr bool kHide = kD > 64 && kKeyTile == 32;
+  constexpr bool kStaged = kFormat != 0 && kD == 256;
+  constexpr int kReadsAhead = kD == 256 ? 2 : kKeyTile == 32 ? 3 : 6;
   constexpr bool kDirect = kFormat == 0;                         // nothing to widen: from memory straight into LDS
-  __shared__ __align__(16) char lds[4 * kTileBytes];             // K and V of two tiles in turn
+  __shared__ __align__(16) char lds[kStaged ? 2 * kTileBytes + 32 * kSource : 4 * kTileBytes];             // K and V of two tiles in turn
   __shared__ int first_bad[kD];                                  // the first key whose V is not finite there, of those that some row does not see
   __shared__ int any_bad;
 
@@ -131,22 +134,32 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   if (tok.count <= 0 || from >= to) return;
 
   // This lane's row, and the last key that it sees; rows behind the last are computed along with it.
-  const int row = 32 * wave + n;
-  int which = (int)((row * group_inverse) >> 16);                // row / G
-  const int head = row - which * a.G;
-  const bool live = which < tok.count;
-  which = min(which, tok.count - 1);
-  const int of_call = (tok.first + which) * a.Hq + kvh * a.G + head;   // T * Hq is below 2^31
-  const int last_key = tok.at + which;
+  struct Row {
+    int of_call, last_key;
+    bool live;
+  };
+  auto row_of = [&](int lane) __attribute__((always_inline)) -> Row {
+    const int row = 32 * wave + (lane & 31), which = (int)((row * group_inverse) >> 16), head = row - which * a.G;   // row / G, row % G
+    const int at = min(which, tok.count - 1);
+    return {(tok.first + at) * a.Hq + kvh * a.G + head, tok.at + at, which < tok.count};   // T * Hq is below 2^31
+  };
+  // kHide: registers are short, and what is cheap to find again is not kept in one over the loop.
+  auto again = [&](int& x) __attribute__((always_inline)) { if constexpr (kHide) asm volatile("" : "+v"(x)); };
+  auto this_lane = [&]() __attribute__((always_inline)) -> int {
+    int here = lane;
+    again(here);
+    return here;
+  };
+  const int last_key = row_of(lane).last_key;
   const int wave_from = __builtin_amdgcn_readlane(last_key, 0), wave_to = __builtin_amdgcn_readlane(last_key, 31);
-  const bool idle = __builtin_amdgcn_readfirstlane(!__any(live));
+  const bool idle = __builtin_amdgcn_readfirstlane(!__any(row_of(lane).live));
 
   bf16x8 q[kSteps];
   const bool negative = a.scale_log2e < 0.f;
   const float scale = fmaxf(__builtin_fabsf(a.scale_log2e), 0x1p-126f);   // masked scores stay -inf with a scale of zero, too
 #pragma unroll
   for (int jj = 0; jj < kSteps; ++jj) {
-    u32x4 x = *(const u32x4*)(a.q + (int64_t)of_call * kD + 16 * jj + 8 * h);
+    u32x4 x = *(const u32x4*)(a.q + (int64_t)row_of(lane).of_call * kD + 16 * jj + 8 * h);
     if (negative) x ^= 0x80008000u;
     q[jj] = __builtin_bit_cast(bf16x8, x);
   }
@@ -185,16 +198,13 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   int window_at = from / kWindowTiles * kWindowTiles;
   Window now = describe(window_at), then = describe(window_at + kWindowTiles);
 
-  auto piece_of = [&](int i) { return (wave * kLoads + i) * 64 + lane; };   // of a tile
+  auto piece_of = [&](int i) __attribute__((always_inline)) { return (wave * kLoads + i) * 64 + this_lane(); };   // of a tile
   // kDirect: the memory unit writes 64 pieces in a row to LDS, so that each lane asks for the piece whose place is its own.
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  int k_from[kLoads], v_from[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int at = piece_of(i) % kOfUnit, t = at / kPerToken, here = at % kPerToken;
-    k_from[i] = t * (kD * kElem) + k_place<kD>(t, here) % (kD * 2);
-    v_from[i] = t * (kD * kElem) + v_place<kD>(t, here) % (kD * 2);
-  }
+  // The unit's bytes for that, of load 0: the others' differ by constants, and in bits that a constant turns over.
+  const int first = piece_of(0) % kOfUnit / kPerToken, here = piece_of(0) % kPerToken;
+  const int k_from = first * (kD * kElem) + k_place<kD>(first, here) % (kD * 2);
+  const int v_from = first * (kD * kElem) + v_place<kD>(first, here) % (kD * 2);
   // A tile on its way: out of memory into registers, from there into LDS.
   u32x4 kr[kLoads], vr[kLoads];
   float ks = 1.f, vs = 1.f;
@@ -218,12 +228,21 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
       ks = __uint_as_float((uint32_t)(both & 0xff) << 23);
       vs = __uint_as_float((uint32_t)(both >> 8) << 23);
     }
+    int k0 = k_from, v0 = v_from;
+    again(k0);
+    again(v0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       if constexpr (kDirect) {
+        constexpr int kTokens = 64 / kPerToken;   // of a load
         const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * 64 * (wave * kLoads + i);
-        load_to_lds(kb, to_lds, k_from[i]);
-        load_to_lds(vb, to_lds + kTileBytes, v_from[i]);
+        load_to_lds(kb, to_lds, (k0 ^ k_place<kD>(kTokens * i, 0) % (kD * 2)) + kTokens * i * kD * kElem);
+        load_to_lds(vb, to_lds + kTileBytes, (v0 ^ v_place<kD>(kTokens * i, 0) % (kD * 2)) + kTokens * i * kD * kElem);
+      } else if constexpr (kStaged) {
+        const uint32_t to_lds = lds_at + 2 * kTileBytes + 16 * 64 * (wave * kLoads + i);
+        const int offset = 16 * (piece_of(i) % kOfUnit);
+        load_to_lds(kb, to_lds, offset);
+        load_to_lds(vb, to_lds + 16 * kSource, offset);
       } else {
         const int offset = 16 * (piece_of(i) % kOfUnit);
         kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, 0));
@@ -298,18 +317,23 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
 
-  // V's operand of keys 16*step .. +15, dims 32*d .. +31
+  // Where this lane reads in LDS: a tile's places differ from these by constants, and in bits that a constant turns over.
+  int k_base = k_place<kD>(n, h), v_base;
   const int v_key = 4 * h + ((lane & 15) >> 2), v_dim = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);   // this lane's part of what 16 lanes transpose
-  auto v_operand = [&](const char* v_lds, int step, int d) -> u32x4 {
+  v_base = v_place<kD>(v_key, v_dim >> 3) + 2 * (v_dim & 7);
+  // V's operand of keys 16*step .. +15, dims 32*d .. +31
+  auto v_operand = [&](const char* v_lds, int base, int step, int d) -> u32x4 {
     typedef __attribute__((address_space(3))) s16x4* Place;
-    const int p = (32 * d + v_dim) >> 3, byte = 2 * (v_dim & 7);
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(v_lds + v_place<kD>(16 * step + v_key, p) + byte));
-    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(v_lds + v_place<kD>(16 * step + 8 + v_key, p) + byte));
+    const char* at = v_lds + (base ^ 64 * (d & 3)) + 256 * (d >> 2) + 16 * step * kD * 2;
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)at);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Place)(at + 8 * kD * 2));
     const u32x2 xx = __builtin_bit_cast(u32x2, x), yy = __builtin_bit_cast(u32x2, y);
     return u32x4{xx.x, xx.y, yy.x, yy.y};
   };
 
   auto attend = [&](const char* k_lds, const char* v_lds, int tile, uint32_t gone) __attribute__((always_inline)) {
+    int k_at = k_base, v_at = v_base;
+    again(k_at);
     f32x16 s[kHalves];
 #pragma unroll
     for (int b = 0; b < kHalves; ++b)
@@ -319,7 +343,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     for (int jj = 0; jj < kSteps; ++jj)
 #pragma unroll
       for (int b = 0; b < kHalves; ++b) {
-        const bf16x8 k = __builtin_bit_cast(bf16x8, *(const u32x4*)(k_lds + k_place<kD>(32 * b + n, 2 * jj + h)));
+        const bf16x8 k = __builtin_bit_cast(bf16x8, *(const u32x4*)(k_lds + (k_at ^ 32 * (jj & 7)) + 256 * (jj >> 3) + 32 * b * kD * 2));
         s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[jj], s[b], 0, 0, 0);
       }
     // some reads ahead of the products, else each waits for its own
@@ -333,6 +357,8 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     const int key0 = kKeyTile * tile;
     if (gone != 0 || key0 + kKeyTile - 1 > wave_from) {
       asm volatile("");   // a branch: most tiles have nothing to mask
+      const int here = this_lane();
+      const int last_key = row_of(here).last_key, h = here >> 5;
 #pragma unroll
       for (int b = 0; b < kHalves; ++b)
 #pragma unroll
@@ -368,12 +394,13 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
 #pragma unroll
       for (int z = 0; z < 8; ++z) p[2 * b + (z >> 2)][z & 3] = pack_bf16(s[b][2 * z], s[b][2 * z + 1]);
     }
+    again(v_at);
     l += kHalves == 2 ? sum[0] + sum[kHalves - 1] : sum[0];
 #pragma unroll
     for (int step = 0; step < 2 * kHalves; ++step)
 #pragma unroll
       for (int d = 0; d < kTiles; ++d)
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v_lds, step, d)), __builtin_bit_cast(bf16x8, p[step]), o[d],
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v_lds, v_at, step, d)), __builtin_bit_cast(bf16x8, p[step]), o[d],
                                                        0, 0, 0);
   };
 
@@ -390,12 +417,23 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
       arrived(tile, v_lds, look);
       __syncthreads();
       if (tile + 1 < to) ask(tile + 1, 1 - kAt);
+    } else if constexpr (kStaged) {
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        kr[i] = *(const u32x4*)(lds + 2 * kTileBytes + 16 * piece_of(i));
+        vr[i] = *(const u32x4*)(lds + 2 * kTileBytes + 16 * kSource + 16 * piece_of(i));
+      }
+      __syncthreads();
+      put(tile, lds, lds + kTileBytes, look);
+      if (tile + 1 < to) ask(tile + 1, 0);
+      __syncthreads();
     } else {
       put(tile, k_lds, v_lds, look);
       if (tile + 1 < to) ask(tile + 1, 0);
       __syncthreads();
     }
-    if (!idle && kKeyTile * tile <= wave_to) attend(k_lds, v_lds, tile, gone);
+    if (!idle && kKeyTile * tile <= wave_to) attend(kStaged ? lds : k_lds, kStaged ? lds + kTileBytes : v_lds, tile, gone);
   };
   for (int tile = from; tile < to; tile += 2) {
     one(tile, std::integral_constant<int, 0>{});
@@ -403,23 +441,26 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
   }
   if (a.id_faults && refused && threadIdx.x == 0) atomicAdd(a.id_faults, refused);
 
-  if (!live) return;
+  const int own = this_lane();
+  const Row row = row_of(own);
+  const int half = own >> 5;
+  if (!row.live) return;
   if (__builtin_expect(any_bad, 0)) {
 #pragma unroll
     for (int d = 0; d < kTiles; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (first_bad[32 * d + 8 * (r >> 2) + 4 * h + (r & 3)] <= last_key) o[d][r] = __builtin_nanf("");
+        if (first_bad[32 * d + 8 * (r >> 2) + 4 * half + (r & 3)] <= row.last_key) o[d][r] = __builtin_nanf("");
   }
   const float total = l + __shfl_xor(l, 32);
-  const int64_t q_row = (int64_t)of_call * kD;
+  const int64_t q_row = (int64_t)row.of_call * kD;
   if (tiles <= a.piece) {
     const float inv = inverse(total, a.out_scale);
 #pragma unroll
     for (int d = 0; d < kTiles; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *(u32x2*)(a.out + q_row + 32 * d + 8 * g + 4 * h) =
+        *(u32x2*)(a.out + q_row + 32 * d + 8 * g + 4 * half) =
             finish_row4(f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]}, inv);
   } else {
     float* part = a.parts + (int64_t)blockIdx.y * a.T * a.Hq * kD + q_row;
@@ -427,8 +468,8 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD)) void prompt_attn_kerne
     for (int d = 0; d < kTiles; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *(f32x4*)(part + 32 * d + 8 * g + 4 * h) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
-    if (h == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + of_call) * 2) = f32x2{m == kLeast ? kNegInf : m, total};
+        *(f32x4*)(part + 32 * d + 8 * g + 4 * half) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+    if (half == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + row.of_call) * 2) = f32x2{m == kLeast ? kNegInf : m, total};
   }
 }
 
@@ -451,7 +492,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
   const int L = min(max(a.context_lens[s], 0), a.max_ctx), n = end - from;
   if (token - from < n - L) return;
   const int last = min(((token - from) / per + 1) * per, n) - 1;     // of its workgroup's tokens
-  constexpr int kKeyTile = prompt_keys(kD);
+  constexpr int kKeyTile = prompt_keys(kD, true);
   const int tiles = (L - n + last + 1 + kKeyTile - 1) / kKeyTile;
   if (tiles <= a.piece) return;
   const int count = (tiles + a.piece - 1) / a.piece;
@@ -481,11 +522,14 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
 template <int kD, int kFormat>
 void launch(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream) {
   const dim3 grid((unsigned)(plan.slots * a.Hkv), plan.pieces), block(kThreads);
-  hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat>), grid, block, 0, stream, a, plan.tokens, (int)plan.slots, 65536u / a.G + 1);
-  if (plan.pieces > 1) {
-    const int heads = 256 / (kD / 4);
-    hipLaunchKernelGGL((prompt_join_kernel<kD>), dim3(a.T, (a.Hq + heads - 1) / heads), dim3(256), 0, stream, a, plan.tokens);
+  const uint32_t group_inverse = 65536u / a.G + 1;
+  if (plan.pieces == 1) {
+    hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat, prompt_keys(kD, false)>), grid, block, 0, stream, a, plan.tokens, (int)plan.slots, group_inverse);
+    return;
   }
+  hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat, prompt_keys(kD, true)>), grid, block, 0, stream, a, plan.tokens, (int)plan.slots, group_inverse);
+  const int heads = 256 / (kD / 4);
+  hipLaunchKernelGGL((prompt_join_kernel<kD>), dim3(a.T, (a.Hq + heads - 1) / heads), dim3(256), 0, stream, a, plan.tokens);
 }
 template <int kD>
 void launch_format(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream) {
@@ -503,11 +547,11 @@ PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
   p.slots = T / p.tokens + S;
   // Few workgroups over long contexts: those are cut.  Into as many pieces as give the least time by this estimate, in us: workgroups in turns of as many
   // as run at once, a tile 2 us (D = 128), a start 3 tiles, and the pieces' rows written and read.
-  const int64_t tiles = ((int64_t)max_ctx + prompt_keys(D) - 1) / prompt_keys(D), groups = p.slots * Hkv, at_once = 256 * prompt_groups(D);
-  const double tile_us = 2.0 * D / 128 * prompt_keys(D) / 64, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
-  p.piece = (int)(tiles > 0 ? tiles : 1);
-  p.pieces = 1;
+  const int keys = prompt_keys(D, true);
+  const int64_t tiles = ((int64_t)max_ctx + keys - 1) / keys, groups = p.slots * Hkv, at_once = 256 * prompt_groups(D, keys);
+  const double tile_us = prompt_groups(D, keys) * (double)D / 128 * keys / 64, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
   double least = 0;
+  p.pieces = 1;
   for (int64_t n = 1; n <= kMaxPieces && 4 * n <= tiles + 3 && (n == 1 || (groups < 2 * at_once && groups * n <= 8 * at_once)); ++n) {
     const int64_t piece = (tiles + n - 1) / n;
     const double us = (double)((groups * n + at_once - 1) / at_once) * (piece + 3) * tile_us + (n > 1 ? 5 + n * join_us : 0);
@@ -517,6 +561,7 @@ PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
       p.pieces = (int)((tiles + piece - 1) / piece);
     }
   }
+  if (p.pieces == 1) p.piece = max_ctx / prompt_keys(D, false) + 1;
   return p;
 }
 
