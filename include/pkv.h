@@ -563,7 +563,11 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
  *   out           device  bf16  [T][Hq][D]; may be q itself, and must not overlap q otherwise, nor the
  *                 pools, scales or tables (PKV_ERR_SHAPE)
  *   shape         host    (partition_size is not used)
- *   workspace     device, >= pkv_prompt_workspace_bytes(), 16-byte aligned; may be NULL when that is 0
+ *   workspace     device, >= pkv_prompt_workspace_bytes(), 16-byte aligned; may be NULL when that is 0;
+ *                 calls that may run at the same time need one each
+ * The report of refused ids counts a refused entry's 16-token units, for each workgroup that meets them: one
+ * for each KV head and for each 128 rows (tokens times heads to a KV head) of the request, 32 where
+ * num_tokens is small for num_seqs (at most num_seqs times what 32 rows hold).
  */
 int pkv_prompt_workspace_bytes(const pkv_attn_shape* shape /* host */, int64_t num_tokens, size_t* out_bytes);
 int paged_prompt_attn(const void* q, const void* k_pool, const void* v_pool,

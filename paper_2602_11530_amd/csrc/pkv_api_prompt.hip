@@ -27,7 +27,7 @@ int check_prompt(const pkv_attn_shape* shape, int64_t tokens, Geometry* g, Promp
   if (tokens == 0 || shape->num_seqs == 0) return PKV_OK;
   *plan = prompt_plan(tokens, shape->num_seqs, shape->num_kv_heads, g->G, shape->head_dim, g->max_ctx);
   // a launch has fewer than 2^32 lanes in a dimension
-  if (plan->slots * shape->num_kv_heads * 2 * plan->rows > UINT32_MAX) return PKV_ERR_SHAPE;
+  if (plan->slots * shape->num_kv_heads * plan->threads > UINT32_MAX) return PKV_ERR_SHAPE;
   if (plan->pieces > 1) *workspace = (size_t)plan->pieces * tokens * shape->num_q_heads * (shape->head_dim + 2) * sizeof(float);
   return PKV_OK;
 }

@@ -427,8 +427,9 @@ struct PromptLaunch {
 };
 // How a launch cuts its work, by what the host knows.
 struct PromptPlan {
-  int rows;         // query rows of a workgroup
-  int tokens;       // that they are of
+  int threads;      // of a workgroup
+  int tokens;       // of its query rows
+  bool alone;       // few rows: each wavefront has all of them and keys of its own
   int64_t slots;    // groups of that many tokens, at most
   int piece, pieces;
 };

@@ -2,15 +2,32 @@
 //
 //   out[i, h] = sum_t softmax_t(scale * q[i, h] . K[t, h / G]) * V[t, h / G]     for t <= p_i, the position of token i
 //
-// A workgroup has the rows (token, head of the group) of some tokens of one request and KV head, 32 to a wavefront, and goes over the keys that
-// the last of them sees, 64 at a time.  K and V of those are staged in LDS as bf16 once for all rows.  Per 32 keys, lane = 32*h + n:
+// A workgroup has the rows (token, head of the group) of some tokens of one request and KV head, 32 to a wavefront, 128 in all, and goes over the keys
+// that the last of them sees, a tile of 32 or 64 at a time.  K and V of a tile are staged in LDS as bf16 once for all rows.  Per 32 keys, lane = 32*h + n:
 //   S^T = K . Q^T   D/16 v_mfma_f32_32x32x16_bf16.  A = K rows, lane (n, h) has the 16 bytes at dims 16*jj + 8*h of key n; B = q, which stays in
 //         registers, lane (n, h) has the same dims of row n.  The result leaves lane (n, h) with row n's scores of keys 8*(r / 4) + 4*h + r % 4.
 //   P     = exp2(score - m), rounded to bf16.  A lane has scores of one row alone, so that maximum, sum and rescale stay in the lane but for one
 //         exchange between the halves when the maximum is raised.
 //   O^T  += V^T . P^T  D/32 times two for 32 keys.  P is the B operand as it came out; A takes dims in rows out of V's rows of dims by
 //         transposing reads of LDS, four keys of 16 dims to 16 lanes, in the order of keys that P has.
-// The running maximum is only raised when a score exceeds it by more than 2^8, as in the decode kernels.
+// The running maximum is only raised when a score exceeds it by more than 2^8, as in the decode kernels.  A weight is one bf16 number here, off by
+// 2^-8 of itself at most, while the decode kernels take two: the second would cost half as many matrix instructions again, and many weights make up a
+// row, so that rows are 0.0021 from those in 64 bits (relative L2) where the rounding of the output alone makes 0.0016.
+//
+// Bound by the matrix unit and the vector unit together: 32 keys at D = 128 are 16 matrix instructions of 32 cycles and 90 vector ones, 16 of them
+// exponentials, in one chain, so that the wavefronts of a SIMD have to cover each other.  The matrix unit is busy for 63 % of one prompt of 8191 tokens
+// (40 heads on 8: 642 us, 1.07 PFLOP/s; a library product of 8192^3 reaches 1.21), for 45 % of sixteen of 100..2000 (300 us, 0.81), where a workgroup has
+// some ten tiles and its chain of four loads before the first (starts, table, unit, first product) is 3 us.
+//   128 rows: LDS is read once for 32 rows and memory once for 128; the LDS unit is active for 23 to 42 % of the time.  One wavefront with 64 rows
+//   has no registers left at D = 128; eight wavefronts were no faster.
+//   Two tiles in LDS in turn, so that a tile's barrier is the only one.  Three: 664 -> 672 us.
+//   bf16 goes from memory straight into LDS, where each lane asks for the piece whose place is its own: no registers in between, no stores to LDS.
+//   e4m3 goes through registers, where it is widened once for all rows; at D = 256, where two workgroups to a unit leave no registers for it, it waits in
+//   LDS as it is, behind a second barrier (e4m3 203 -> 156 us, eight prompts of 200..1500 tokens).
+//   D = 256 in 256 registers, two workgroups to a unit, instead of one with 300: 194 -> 146 us.
+//   Few rows (kAlone): where a request has rows for one wavefront, three would wait for it.  All four take them, each with every fourth tile, in LDS of its
+//   own without barriers, nontemporal as nobody else reads it, and join in the end.  4 tokens of each of 32 requests with 1000..8000 behind them, memory's
+//   case (592 MB): 125 -> 114 us (5.2 TB/s), 11 of them by the loads' kind; over e4m3 85 -> 64, of 200 requests 713 -> 636 (6.0 TB/s) and 448 -> 338.
 #include "attn_partial.h"
 #include "pkv_kernels.h"
 
@@ -33,10 +50,12 @@ constexpr int kMfma = 0x8, kDsRead = 0x100;       // kinds of instructions, for 
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kMaxPieces = 64;                    // of a context
-// Keys of a tile, where contexts are cut and where they are whole.
+// Keys of a tile, where contexts are cut and where they are whole.  With 32 at D = 128 three workgroups go on a unit instead of two: sixteen prompts of
+// 100..2000 tokens 324 -> 298 us, over e4m3 335 -> 314; contexts that are cut stay long for their workgroups: 512 tokens behind 32000 371 us
+// with 64 and 388 with 32.
 __host__ __device__ constexpr int prompt_keys(int D, bool cut) { return D == 256 || (D == 128 && !cut) ? 32 : 64; }
 // Workgroups that run on a compute unit at once, by their registers and LDS.
-constexpr int prompt_groups(int D, int keys) { return D == 64 ? 4 : D == 128 && keys == 32 ? 3 : 2; }
+constexpr int prompt_groups(int D, int keys, bool alone) { return D == 64 ? 4 : alone ? 256 / D : D == 128 && keys == 32 ? 3 : 2; }
 
 // A workgroup's tokens: `first` to `first + count` of the call, of request s, at position `at` and on.
 struct Tokens {
@@ -85,7 +104,13 @@ __device__ __forceinline__ u32x2 widen(uint32_t w, float scale) {
 
 // 64 lanes' pieces of a buffer, zeros out of its bounds, to 1 KiB in a row of LDS from `to` on.  An opaque instruction: the compiler would wait for it
 // before every read of LDS that follows, whatever it reads.  Who asks waits for what was asked for, and meets the others, before anyone reads it.
+// kOnce: nobody else reads it, and it need not stay in the caches.
+template <bool kOnce>
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t b, uint32_t to, int offset) {
+  if constexpr (kOnce) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
+    return;
+  }
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
 }
 
@@ -102,8 +127,8 @@ template <int kD> __device__ __forceinline__ int v_place(int t, int p) {
   return (t * kPieces + (p ^ (turn << 2))) * 16;
 }
 
-template <int kD, int kFormat, int kKeyTile>
-__global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_attn_kernel(PromptLaunch a, int per, int slots, uint32_t group_inverse) {
+template <int kD, int kFormat, int kKeyTile, bool kAlone>
+__global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void prompt_attn_kernel(PromptLaunch a, int per, int slots, uint32_t group_inverse) {
   constexpr int kSteps = kD / 16, kTiles = kD / 32;
   constexpr int kHalves = kKeyTile / 32;
   constexpr int kUnits = kKeyTile / kBlockTokens;                // of a tile
@@ -111,17 +136,20 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
   constexpr int kTileBytes = kKeyTile * kD * 2;
   constexpr int kElem = kFormat == 0 ? 2 : 1;
   constexpr int kSource = kKeyTile * kD * kElem / 16;            // 16-byte pieces of a tile as the pool has it
-  constexpr int kLoads = kSource / kThreads;                     // of a lane
+  constexpr int kLoads = kSource / (kAlone ? 64 : kThreads);     // of a lane
   constexpr int kPerToken = kD * kElem / 16;
   constexpr int kOfUnit = kPerToken * kBlockTokens;
-  static_assert(kLoads * kThreads == kSource && kOfUnit % (64 * kLoads) == 0, "a wavefront loads pieces of one unit");
-  constexpr bool kHide = kD > 64 && kKeyTile == 32;
-  constexpr bool kStaged = kFormat != 0 && kD == 256;
-  constexpr int kReadsAhead = kD == 256 ? 2 : kKeyTile == 32 ? 3 : 6;
+  constexpr int kOwn = kAlone ? kUnits : 1, kEach = kLoads / kOwn;   // units that a wavefront loads from, its loads of one
+  static_assert(kEach * kOwn * (kAlone ? 64 : kThreads) == kSource && kOfUnit % (64 * kEach) == 0, "whole units, or pieces of one");
   constexpr bool kDirect = kFormat == 0;                         // nothing to widen: from memory straight into LDS
-  __shared__ __align__(16) char lds[kStaged ? 2 * kTileBytes + 32 * kSource : 4 * kTileBytes];             // K and V of two tiles in turn
+  constexpr bool kStaged = kFormat != 0 && kD == 256 && !kAlone;            // on its way to registers through LDS
+  constexpr bool kHide = kD > 64 && kKeyTile == 32 && !kAlone;              // registers are short: what is cheap to find again is not kept in one over the loop
+  constexpr int kReadsAhead = kAlone ? 4 : kD == 256 ? 2 : kKeyTile == 32 ? 3 : 6;   // of LDS in the first product, as many as there are registers for
+  // K and V of two tiles in turn, or of one as bf16 and behind it of the next as it is
+  __shared__ __align__(16) char lds[kAlone ? 2 * kWaves * kTileBytes : kStaged ? 2 * kTileBytes + 32 * kSource : 4 * kTileBytes];
   __shared__ int first_bad[kD];                                  // the first key whose V is not finite there, of those that some row does not see
   __shared__ int any_bad;
+  [[maybe_unused]] __shared__ float stats_of[kAlone ? kWaves : 1][2][32];   // kAlone: of a wavefront's rows
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -139,11 +167,11 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
     bool live;
   };
   auto row_of = [&](int lane) __attribute__((always_inline)) -> Row {
-    const int row = 32 * wave + (lane & 31), which = (int)((row * group_inverse) >> 16), head = row - which * a.G;   // row / G, row % G
+    const int row = (kAlone ? 0 : 32 * wave) + (lane & 31), which = (int)((row * group_inverse) >> 16), head = row - which * a.G;   // row / G, row % G
     const int at = min(which, tok.count - 1);
     return {(tok.first + at) * a.Hq + kvh * a.G + head, tok.at + at, which < tok.count};   // T * Hq is below 2^31
   };
-  // kHide: registers are short, and what is cheap to find again is not kept in one over the loop.
+  // With kHide the compiler does not know that this is the same number as before.
   auto again = [&](int& x) __attribute__((always_inline)) { if constexpr (kHide) asm volatile("" : "+v"(x)); };
   auto this_lane = [&]() __attribute__((always_inline)) -> int {
     int here = lane;
@@ -198,7 +226,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
   int window_at = from / kWindowTiles * kWindowTiles;
   Window now = describe(window_at), then = describe(window_at + kWindowTiles);
 
-  auto piece_of = [&](int i) __attribute__((always_inline)) { return (wave * kLoads + i) * 64 + this_lane(); };   // of a tile
+  auto piece_of = [&](int i) __attribute__((always_inline)) { return ((kAlone ? 0 : wave * kLoads) + i) * 64 + this_lane(); };   // of a tile
   // kDirect: the memory unit writes 64 pieces in a row to LDS, so that each lane asks for the piece whose place is its own.
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   // The unit's bytes for that, of load 0: the others' differ by constants, and in bits that a constant turns over.
@@ -207,7 +235,9 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
   const int v_from = first * (kD * kElem) + v_place<kD>(first, here) % (kD * 2);
   // A tile on its way: out of memory into registers, from there into LDS.
   u32x4 kr[kLoads], vr[kLoads];
-  float ks = 1.f, vs = 1.f;
+  float ks[kOwn], vs[kOwn];   // of the units that it is from
+#pragma unroll
+  for (int x = 0; x < kOwn; ++x) ks[x] = vs[x] = 1.f;
   uint32_t unmapped = 0;      // of the tile that was asked for last, a bit for each unit that is not there
   auto ask = [&](int tile, int at_place) {
     if (tile >= window_at + kWindowTiles) {
@@ -217,43 +247,47 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
     }
     const int u0 = kUnits * (tile - window_at);
     unmapped = (uint32_t)(now.gone >> u0) & ((1 << kUnits) - 1);
-    const int u = u0 + wave * kLoads * 64 / kOfUnit;
-    const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(now.at >> 32), u) << 32 |
-                        (uint32_t)__builtin_amdgcn_readlane((int)now.at, u);
-    const int rows = now.gone >> u & 1 ? 0 : min(kBlockTokens, context - (kUnits * window_at + u) * kBlockTokens), bytes = rows * (kD * kElem);
-    const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, kRawBuffer);
-    const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)(at + v_behind), 0, bytes, kRawBuffer);
-    if constexpr (kFormat == kBlkPools) {
-      const int both = __builtin_amdgcn_readlane(now.scales, u);
-      ks = __uint_as_float((uint32_t)(both & 0xff) << 23);
-      vs = __uint_as_float((uint32_t)(both >> 8) << 23);
-    }
-    int k0 = k_from, v0 = v_from;
-    again(k0);
-    again(v0);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      if constexpr (kDirect) {
-        constexpr int kTokens = 64 / kPerToken;   // of a load
-        const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * 64 * (wave * kLoads + i);
-        load_to_lds(kb, to_lds, (k0 ^ k_place<kD>(kTokens * i, 0) % (kD * 2)) + kTokens * i * kD * kElem);
-        load_to_lds(vb, to_lds + kTileBytes, (v0 ^ v_place<kD>(kTokens * i, 0) % (kD * 2)) + kTokens * i * kD * kElem);
-      } else if constexpr (kStaged) {
-        const uint32_t to_lds = lds_at + 2 * kTileBytes + 16 * 64 * (wave * kLoads + i);
-        const int offset = 16 * (piece_of(i) % kOfUnit);
-        load_to_lds(kb, to_lds, offset);
-        load_to_lds(vb, to_lds + 16 * kSource, offset);
-      } else {
-        const int offset = 16 * (piece_of(i) % kOfUnit);
-        kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, 0));
-        vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, 0));
+    for (int x = 0; x < kOwn; ++x) {
+      const int u = u0 + (kAlone ? x : wave * kLoads * 64 / kOfUnit);
+      const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(now.at >> 32), u) << 32 |
+                          (uint32_t)__builtin_amdgcn_readlane((int)now.at, u);
+      const int rows = now.gone >> u & 1 ? 0 : min(kBlockTokens, context - (kUnits * window_at + u) * kBlockTokens), bytes = rows * (kD * kElem);
+      const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, kRawBuffer);
+      const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc((void*)(at + v_behind), 0, bytes, kRawBuffer);
+      if constexpr (kFormat == kBlkPools) {
+        const int both = __builtin_amdgcn_readlane(now.scales, u);
+        ks[x] = __uint_as_float((uint32_t)(both & 0xff) << 23);
+        vs[x] = __uint_as_float((uint32_t)(both >> 8) << 23);
+      }
+      int k0 = k_from, v0 = v_from;
+      again(k0);
+      again(v0);
+#pragma unroll
+      for (int y = 0; y < kEach; ++y) {
+        const int i = x * kEach + y;
+        if constexpr (kDirect) {
+          constexpr int kTokens = 64 / kPerToken;   // of a load
+          const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * 64 * ((kAlone ? 0 : wave * kLoads) + i);
+          load_to_lds<kAlone>(kb, to_lds, (k0 ^ k_place<kD>(kTokens * y, 0) % (kD * 2)) + kTokens * y * kD * kElem);
+          load_to_lds<kAlone>(vb, to_lds + kTileBytes, (v0 ^ v_place<kD>(kTokens * y, 0) % (kD * 2)) + kTokens * y * kD * kElem);
+        } else if constexpr (kStaged) {
+          const uint32_t to_lds = lds_at + 2 * kTileBytes + 16 * 64 * (wave * kLoads + i);
+          const int offset = 16 * (piece_of(i) % kOfUnit);
+          load_to_lds<kAlone>(kb, to_lds, offset);
+          load_to_lds<kAlone>(vb, to_lds + 16 * kSource, offset);
+        } else {
+          const int offset = 16 * (piece_of(i) % kOfUnit);
+          kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, kAlone ? 2 : 0));
+          vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, kAlone ? 2 : 0));
+        }
       }
     }
   };
   // What is not finite in V of keys that some row may not see does not go through the matrix product, where a weight of zero does not silence it: it
   // is held back, and the rows that see its key become NaN there in the end.
   auto hold_back = [&](int i, int tile, int t, int p) {
-    constexpr int kEach = 16 / kElem;
+    constexpr int kValues = 16 / kElem;
     bool bad = false;
 #pragma unroll
     for (int z = 0; z < 4; ++z) {
@@ -261,15 +295,15 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
       if constexpr (kFormat == 0) bad |= (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
       else bad |= (w & 0x7fu) == 0x7fu || (w & 0x7f00u) == 0x7f00u || (w & 0x7f0000u) == 0x7f0000u || (w & 0x7f000000u) == 0x7f000000u;
     }
-    const bool all = kFormat == kBlkPools && !(vs < kTooLarge);
+    const bool all = kFormat == kBlkPools && !(vs[i / kEach] < kTooLarge);
     if (!bad && !all) return;
     any_bad = 1;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
+    for (int e = 0; e < kValues; ++e) {
       const int shift = 8 * kElem * (e % (4 / kElem));
       const uint32_t mask = kFormat == 0 ? 0x7f80u : 0x7fu;
       if (all || ((vr[i][e * kElem / 4] >> shift) & mask) == mask) {
-        atomicMin(&first_bad[kEach * p + e], kKeyTile * tile + t);
+        atomicMin(&first_bad[kValues * p + e], kKeyTile * tile + t);
         vr[i][e * kElem / 4] &= ~((kFormat == 0 ? 0xffffu : 0xffu) << shift);
       }
     }
@@ -289,11 +323,11 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
     }
   };
   auto put = [&](int tile, char* k_lds, char* v_lds, bool look) {
-    const float v_by = look && !(vs < kTooLarge) ? 1.f : vs;     // held back, all of it
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int piece = piece_of(i);
       const int t = piece / kPerToken, p = piece % kPerToken;
+      const float k_by = ks[i / kEach], v_by = look && !(vs[i / kEach] < kTooLarge) ? 1.f : vs[i / kEach];   // held back, all of it
       if (look) hold_back(i, tile, t, p);
       if constexpr (kFormat == 0) {
         *(u32x4*)(k_lds + k_place<kD>(t, p)) = kr[i];
@@ -301,7 +335,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
       } else {
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const u32x2 k0 = widen(kr[i][2 * z], ks), k1 = widen(kr[i][2 * z + 1], ks);
+          const u32x2 k0 = widen(kr[i][2 * z], k_by), k1 = widen(kr[i][2 * z + 1], k_by);
           *(u32x4*)(k_lds + k_place<kD>(t, 2 * p + z)) = u32x4{k0.x, k0.y, k1.x, k1.y};
           const u32x2 v0 = widen(vr[i][2 * z], v_by), v1 = widen(vr[i][2 * z + 1], v_by);
           *(u32x4*)(v_lds + v_place<kD>(t, 2 * p + z)) = u32x4{v0.x, v0.y, v1.x, v1.y};
@@ -407,6 +441,29 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
   for (int d = threadIdx.x; d < kD; d += kThreads) first_bad[d] = INT32_MAX;
   if (threadIdx.x == 0) any_bad = 0;
   __syncthreads();
+  if constexpr (kAlone) {
+    // Every wavefront has all rows and every fourth tile, in LDS of its own: nobody waits for another before the end.
+    char *k_lds = lds + 2 * wave * kTileBytes, *v_lds = k_lds + kTileBytes;
+    const int first_tile = from + wave;
+    if (first_tile < to) ask(first_tile, wave);
+    for (int tile = first_tile; tile < to; tile += kWaves) {
+      const uint32_t gone = unmapped;
+      const bool look = kKeyTile * tile + kKeyTile - 1 > tok.at;
+      if constexpr (kDirect) {
+        arrived(tile, v_lds, look);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        attend(k_lds, v_lds, tile, gone);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // has read the tile
+        if (tile + kWaves < to) ask(tile + kWaves, wave);
+      } else {
+        put(tile, k_lds, v_lds, look);
+        if (tile + kWaves < to) ask(tile + kWaves, wave);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+        attend(k_lds, v_lds, tile, gone);
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+      }
+    }
+  } else {
   ask(from, 0);
   auto one = [&](int tile, auto at_place) __attribute__((always_inline)) {
     constexpr int kAt = decltype(at_place)::value;
@@ -418,7 +475,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
       __syncthreads();
       if (tile + 1 < to) ask(tile + 1, 1 - kAt);
     } else if constexpr (kStaged) {
-      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+      asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // a wavefront reads what it asked for itself
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         kr[i] = *(const u32x4*)(lds + 2 * kTileBytes + 16 * piece_of(i));
@@ -439,7 +496,41 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
     one(tile, std::integral_constant<int, 0>{});
     if (tile + 1 < to) one(tile + 1, std::integral_constant<int, 1>{});
   }
+  }
   if (a.id_faults && refused && threadIdx.x == 0) atomicAdd(a.id_faults, refused);
+  if constexpr (kAlone) {
+    // The rows of four wavefronts into the first one's, where a lane finds its own numbers.
+    l += __shfl_xor(l, 32);
+    f32x4* mine = (f32x4*)(lds + 2 * wave * kTileBytes) + lane;
+    static_assert(2 * kTileBytes >= kTiles * 16 * 64 * 4);
+    if (wave > 0) {
+#pragma unroll
+      for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) mine[(4 * d + g) * 64] = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+      if (h == 0) {
+        stats_of[wave][0][n] = m;
+        stats_of[wave][1][n] = l;
+      }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 1; w < kWaves; ++w) {
+      const float other = stats_of[w][0][n], most = fmaxf(m, other);
+      const float mine_by = __builtin_amdgcn_exp2f(m - most), other_by = __builtin_amdgcn_exp2f(other - most);
+      const f32x4* its = (const f32x4*)(lds + 2 * w * kTileBytes) + lane;
+      m = most;
+      l = l * mine_by + stats_of[w][1][n] * other_by;
+#pragma unroll
+      for (int d = 0; d < kTiles; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 x = its[(4 * d + g) * 64];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) o[d][4 * g + z] = o[d][4 * g + z] * mine_by + x[z] * other_by;
+        }
+    }
+  }
 
   const int own = this_lane();
   const Row row = row_of(own);
@@ -452,7 +543,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
       for (int r = 0; r < 16; ++r)
         if (first_bad[32 * d + 8 * (r >> 2) + 4 * half + (r & 3)] <= row.last_key) o[d][r] = __builtin_nanf("");
   }
-  const float total = l + __shfl_xor(l, 32);
+  const float total = kAlone ? l : l + __shfl_xor(l, 32);
   const int64_t q_row = (int64_t)row.of_call * kD;
   if (tiles <= a.piece) {
     const float inv = inverse(total, a.out_scale);
@@ -475,7 +566,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile)) void prompt_
 
 // The rows of contexts that were cut, from their pieces: D / 4 lanes to a row.
 template <int kD>
-__global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int per) {
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int per, int keys) {
   constexpr int kLanes = kD / 4, kAtOnce = 4;
   const int token = blockIdx.x;
   // the slot of a token is found the way its workgroup was: all of its request's slots begin at or before it
@@ -492,8 +583,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
   const int L = min(max(a.context_lens[s], 0), a.max_ctx), n = end - from;
   if (token - from < n - L) return;
   const int last = min(((token - from) / per + 1) * per, n) - 1;     // of its workgroup's tokens
-  constexpr int kKeyTile = prompt_keys(kD, true);
-  const int tiles = (L - n + last + 1 + kKeyTile - 1) / kKeyTile;
+  const int tiles = (L - n + last + 1 + keys - 1) / keys;
   if (tiles <= a.piece) return;
   const int count = (tiles + a.piece - 1) / a.piece;
   const int64_t rows = (int64_t)a.T * a.Hq;
@@ -519,17 +609,21 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
   }
 }
 
+template <int kD, int kFormat, int kKeyTile, bool kAlone>
+void launch_tiles(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream) {
+  const dim3 grid((unsigned)(plan.slots * a.Hkv), plan.pieces);
+  hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat, kKeyTile, kAlone>), grid, dim3(kThreads), 0, stream, a, plan.tokens, (int)plan.slots,
+                     65536u / a.G + 1);
+}
 template <int kD, int kFormat>
 void launch(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream) {
-  const dim3 grid((unsigned)(plan.slots * a.Hkv), plan.pieces), block(kThreads);
-  const uint32_t group_inverse = 65536u / a.G + 1;
-  if (plan.pieces == 1) {
-    hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat, prompt_keys(kD, false)>), grid, block, 0, stream, a, plan.tokens, (int)plan.slots, group_inverse);
-    return;
-  }
-  hipLaunchKernelGGL((prompt_attn_kernel<kD, kFormat, prompt_keys(kD, true)>), grid, block, 0, stream, a, plan.tokens, (int)plan.slots, group_inverse);
+  if (plan.alone) launch_tiles<kD, kFormat, 32, true>(a, plan, stream);
+  else if (plan.pieces == 1) launch_tiles<kD, kFormat, prompt_keys(kD, false), false>(a, plan, stream);
+  else launch_tiles<kD, kFormat, prompt_keys(kD, true), false>(a, plan, stream);
+  if (plan.pieces == 1) return;
   const int heads = 256 / (kD / 4);
-  hipLaunchKernelGGL((prompt_join_kernel<kD>), dim3(a.T, (a.Hq + heads - 1) / heads), dim3(256), 0, stream, a, plan.tokens);
+  hipLaunchKernelGGL((prompt_join_kernel<kD>), dim3(a.T, (a.Hq + heads - 1) / heads), dim3(256), 0, stream, a, plan.tokens,
+                     plan.alone ? 32 : prompt_keys(kD, true));
 }
 template <int kD>
 void launch_format(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream) {
@@ -542,26 +636,30 @@ void launch_format(const PromptLaunch& a, const PromptPlan& plan, hipStream_t st
 
 PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
   PromptPlan p;
-  p.rows = 32 * kWaves;
-  p.tokens = p.rows / G;
+  p.threads = kThreads;
+  p.alone = T <= (int64_t)S * (32 / G);   // what a request has fits a wavefront, if they have alike
+  p.tokens = (p.alone ? 32 : 32 * kWaves) / G;
   p.slots = T / p.tokens + S;
   // Few workgroups over long contexts: those are cut.  Into as many pieces as give the least time by this estimate, in us: workgroups in turns of as many
-  // as run at once, a tile 2 us (D = 128), a start 3 tiles, and the pieces' rows written and read.
-  const int keys = prompt_keys(D, true);
-  const int64_t tiles = ((int64_t)max_ctx + keys - 1) / keys, groups = p.slots * Hkv, at_once = 256 * prompt_groups(D, keys);
-  const double tile_us = prompt_groups(D, keys) * (double)D / 128 * keys / 64, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
+  // as run at once, a tile 2 us with D = 128, a start 3 tiles, and the pieces' rows written and read.  A call that fills the card twice is not cut
+  // (eight prompts of D = 256 in pieces 245 us, whole 206), and no more workgroups are made than eight times fill it (drafts of 32 requests: with a stop at
+  // two times 144 us, at eight 125).  With few rows memory is the bound: as many pieces as fill the card once, where contexts are as long as they may be;
+  // a request has one group of rows there, of the slots that are kept for more.  Pieces of them, drafts of 8 requests, us: 1 89, 2 54, 4 50, 8 40, 16 45.
+  const int keys = p.alone ? 32 : prompt_keys(D, true);
+  const int64_t tiles = ((int64_t)max_ctx + keys - 1) / keys, groups = (p.alone ? S : p.slots) * Hkv, at_once = 256 * prompt_groups(D, keys, p.alone);
+  const double tile_us = p.alone ? 0.5 : prompt_groups(D, keys, false) * (double)D / 128 * keys / 64, join_us = (double)T * G * Hkv * (D + 2) * 8 / 5e6;
   double least = 0;
   p.pieces = 1;
   for (int64_t n = 1; n <= kMaxPieces && 4 * n <= tiles + 3 && (n == 1 || (groups < 2 * at_once && groups * n <= 8 * at_once)); ++n) {
     const int64_t piece = (tiles + n - 1) / n;
-    const double us = (double)((groups * n + at_once - 1) / at_once) * (piece + 3) * tile_us + (n > 1 ? 5 + n * join_us : 0);
+    const double us = (double)((groups * n + at_once - 1) / at_once) * (piece + 3) * tile_us + (n > 1 ? 5 + n * (join_us + (p.alone ? 0.3 : 0)) : 0);
     if (n == 1 || us < least) {
       least = us;
       p.piece = (int)piece;
       p.pieces = (int)((tiles + piece - 1) / piece);
     }
   }
-  if (p.pieces == 1) p.piece = max_ctx / prompt_keys(D, false) + 1;
+  if (p.pieces == 1) p.piece = max_ctx / (p.alone ? 32 : prompt_keys(D, false)) + 1;
   return p;
 }
 

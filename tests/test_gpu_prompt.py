@@ -345,3 +345,58 @@ def test_one_token_after_another_as_a_program_goes():
             assert np.array_equal(getattr(p, name + "_dev").cpu().numpy(), getattr(p, name + "_bits"))
             assert np.array_equal(getattr(p, name + "s_dev").cpu().numpy(), getattr(p, name + "_scales"))
     assert any(not np.array_equal(fresh[n], getattr(p, n)) for n in fresh)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,hkv,dim,block", [(8, 2, 128, 16), (16, 2, 64, 64), (6, 2, 256, 32), (13, 1, 128, 32)])
+@pytest.mark.parametrize("longest", [40, 3000])
+def test_few_rows(kind, hq, hkv, dim, block, longest):
+    """A few tokens of each request, of one more than a wavefront has rows for, of one none; contexts from nothing to long."""
+    rng = np.random.default_rng(hq + longest)
+    new = rng.integers(1, 3, 24)
+    new[3], new[7] = 45 * 2 * hkv // hq + 1, 0
+    cached = rng.integers(0, longest, 24)
+    cached[[0, 5, 9]] = 0, 31, 127
+    b = make_batch(cached, new, hq, hkv, dim, block, hq + dim, lead=1, tail=2)
+    assert b.tokens <= 24 * (32 * hkv // hq)
+    both(b, pools_of(b, kind))
+
+
+@pytest.mark.expects_id_faults
+@pytest.mark.parametrize("kind", KINDS)
+def test_few_rows_with_blocks_outside_the_pool(id_faults, kind):
+    b = make_batch([500, 16, 0, 300], [4, 3, 2, 1], 8, 2, 128, 16, 21)
+    p = pools_of(b, kind)
+    b.tables[0][1], b.tables[0][30], b.tables[2][0], b.tables[3][9] = -1, b.num_blocks, 2 ** 31 - 1, -2 ** 31
+    got = run_prompt(b, p)
+    check(b, got, *plain_prompt(b, p))
+    assert (got[b.starts[2]:b.starts[3]] == 0).all()
+    assert int(id_faults.item()) == 4 * 2         # a unit each, for each KV head
+
+
+def test_few_rows_without_finite_scales():
+    b = make_batch([70, 200, 30], [3, 4, 2], 4, 2, 128, 16, 22)
+    p = pools_of(b, "blk")
+    p.v_scales[b.tables[0][4], 1], p.v_scales[b.tables[1][12], 0] = 255, 254      # tokens 64 to 79 of 73, 192 to 207 of 204
+    p.v_bits[b.tables[1][12], 0] = 0x7E
+    upload(p)
+    got = wl.bf16_bits_to_f64(run_prompt(b, p)).reshape(b.q_bits.shape)
+    bad = np.zeros(got.shape, bool)
+    bad[:3, 2:], bad[3:7, :2] = True, True
+    assert np.isfinite(got[~bad]).all() and not np.isfinite(got[bad]).any()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_few_rows_are_those_of_many(kind):
+    """The same tokens beside a request that has many: other workgroups, rows within twice the tolerance of each other."""
+    b = make_batch([900, 40], [3, 2], 8, 2, 128, 16, 23)
+    p = pools_of(b, kind)
+    few = wl.bf16_bits_to_f64(run_prompt(b, p)).reshape(b.q_bits.shape)
+    want, off, has = plain_prompt(b, p)
+    b.tables = np.concatenate([b.tables, b.tables[:1]])
+    b.new, b.lens = np.r_[b.new, 500].astype(np.int32), np.r_[b.lens, 500].astype(np.int32)
+    b.starts = np.r_[b.starts, b.starts[-1] + 500].astype(np.int32)
+    b.tokens += 500
+    b.q_bits = np.concatenate([b.q_bits, wl.normal_bf16(b.rng, (500, 8, 128))])
+    many = wl.bf16_bits_to_f64(run_prompt(b, p)).reshape(b.q_bits.shape)[:5]
+    assert (np.abs(few - want) <= off).all() and (np.abs(many - want) <= off).all() and has.all()
