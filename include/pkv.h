@@ -453,8 +453,9 @@ int kv_append_fp4(const void* k_new, const void* v_new, void* k_pool, void* v_po
  *   byte = e4m3(e4m3(byte) * old / new).
  * New values are stored as byte = e4m3(x / scale), round to nearest even, zeros keeping
  * their sign, magnitudes beyond 448 * scale (infinity, or above 448 * 2^119) held there,
- * NaN as NaN.  K and V have their own scales.  Of a block that other requests have in
- * their tables no token may be appended to (unchecked), as for every append.
+ * NaN as NaN.  K and V have their own scales.  To a block that other requests have in
+ * their tables no token may be appended (unchecked), as for every append.
+ * max_context_len, or MAXB*B if that is 0, is at most 2^31 - 4097.
  * Everything else as for kv_append.
  *
  *   k_pool, v_pool      device  e4m3  [NB][Hkv][B][D]
@@ -562,7 +563,7 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
  *   num_tokens    T, 0..2^24-1
  *   out           device  bf16  [T][Hq][D]; may be q itself, and must not overlap q otherwise, nor the
  *                 pools, scales or tables (PKV_ERR_SHAPE)
- *   shape         host    (partition_size is not used)
+ *   shape         host    (partition_size is not used); max_context_len, or MAXB*B if that is 0, at most 2^31 - 4097
  *   workspace     device, >= pkv_prompt_workspace_bytes(), 16-byte aligned; may be NULL when that is 0;
  *                 calls that may run at the same time need one each
  * The report of refused ids counts a refused entry's 16-token units, for each workgroup that meets them: one

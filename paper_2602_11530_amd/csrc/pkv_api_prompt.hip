@@ -22,7 +22,7 @@ uint64_t scales_bytes(const pkv_attn_shape* sh) { return (uint64_t)sh->num_pool_
 int check_prompt(const pkv_attn_shape* shape, int64_t tokens, Geometry* g, PromptPlan* plan, size_t* workspace) {
   const int rc = check_shape(shape, g);
   if (rc != PKV_OK) return rc;
-  if (tokens < 0 || tokens > kMaxTokens) return PKV_ERR_SHAPE;
+  if (tokens < 0 || tokens > kMaxTokens || g->max_ctx > kMaxTiledContext) return PKV_ERR_SHAPE;
   *workspace = 0;
   if (tokens == 0 || shape->num_seqs == 0) return PKV_OK;
   *plan = prompt_plan(tokens, shape->num_seqs, shape->num_kv_heads, g->G, shape->head_dim, g->max_ctx);

@@ -124,6 +124,7 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
   const int rc = prepare_rope(q, k, v, q_norm, k_norm, cos_sin, q_out, k_pool, v_pool, block_tables, context_lens, token_starts, kBlkPools, 1.f,
                               1.f, rope, shape, true, &a, &empty);
   if (rc != PKV_OK || empty) return rc;
+  if (a.max_ctx > kMaxTiledContext) return PKV_ERR_SHAPE;
   if (!k_scales || !v_scales) return PKV_ERR_NULL;
   if (misaligned16(k_scales) || misaligned16(v_scales)) return PKV_ERR_ALIGN;
   return launch_status(launch_kv_append_blk(a, k_scales, v_scales, static_cast<hipStream_t>(stream)));

@@ -32,6 +32,9 @@ struct Geometry {
 // fewer; the rest takes those of further layers of a launch, or rows (launch_layer).
 inline int64_t record_slots(int S, int Hkv) { return (int64_t)Hkv * S + kStreamWaves; }
 
+// Longest context of the calls for prompts and of appends with block scales, whose device code numbers positions some tiles behind a context's end.
+constexpr int kMaxTiledContext = INT32_MAX - 4096;
+
 inline int check_shape(const pkv_attn_shape* sh, Geometry* g) {
   if (!sh) return PKV_ERR_NULL;
   if (sh->num_seqs < 0 || sh->num_seqs > kMaxSeqs) return PKV_ERR_SHAPE;

@@ -211,3 +211,21 @@ def test_numbers_of_tokens(monkeypatch, name, module):
     args[at] = 5.0
     with pytest.raises(TypeError):
         getattr(pkv, name)(*args, 0)
+
+
+def test_longest_contexts():
+    """Positions some tiles behind the end of a context are numbered in 32 bits."""
+    def shape(most):
+        return pkv.make_shape(1, 1, 1, 2 ** 27 - 1, 128, max_context_len=most)
+    longest = 2 ** 31 - 4097
+    assert pkv.pkv_prompt_workspace_bytes(shape(longest), 1) > 0
+    for most in (longest + 1, 0):
+        with pytest.raises(pkv.PkvError) as e:
+            pkv.pkv_prompt_workspace_bytes(shape(most), 1)
+        assert e.value.status == pkv.PKV_ERR_SHAPE
+        for name in ("paged_prompt_attn", "paged_prompt_attn_fp8kv", "paged_prompt_attn_fp8blk"):
+            assert prompt(name, shape=shape(most), n=1) == pkv.PKV_ERR_SHAPE
+        assert pkv.lib().kv_append_fp8blk(MIB, 2 * MIB, 3 * MIB, 4 * MIB, 5 * MIB, 6 * MIB, 7 * MIB, 8 * MIB, ref(shape(most)), None) == pkv.PKV_ERR_SHAPE
+        rope = pkv.make_rope(1, 0, 0)
+        assert pkv.lib().kv_rope_append_fp8blk(None, MIB, 2 * MIB, None, None, None, None, 3 * MIB, 4 * MIB, 5 * MIB, 6 * MIB, 7 * MIB, 8 * MIB, 9 * MIB,
+                                               ctypes.byref(rope), ref(shape(most)), None) == pkv.PKV_ERR_SHAPE
