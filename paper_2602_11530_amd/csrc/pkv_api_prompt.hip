@@ -89,6 +89,7 @@ int attend_prompt(const void* q, const void* k_pool, const void* v_pool, const u
   a.NB = (int)shape->num_pool_blocks;
   a.piece = plan.piece;
   a.pieces = plan.pieces;
+  a.ordered = plan.ordered && token_starts;
   return launch_status(launch_prompt(a, plan, static_cast<hipStream_t>(stream)));
 }
 

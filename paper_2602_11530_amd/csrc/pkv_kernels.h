@@ -424,6 +424,7 @@ struct PromptLaunch {
   int MAXB, log_block, max_ctx, NB;
   int piece;                            // tiles of keys that a workgroup takes at most
   int pieces;                           // of a context, by the bounds
+  bool ordered;                         // workgroups with most keys come first
 };
 // How a launch cuts its work, by what the host knows.
 struct PromptPlan {
@@ -432,6 +433,7 @@ struct PromptPlan {
   bool alone;       // few rows: each wavefront has all of them and keys of its own
   int64_t slots;    // groups of that many tokens, at most
   int piece, pieces;
+  bool ordered;     // up to 64 requests: workgroups with most keys come first
 };
 PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx);
 hipError_t launch_prompt(const PromptLaunch& a, const PromptPlan& plan, hipStream_t stream);

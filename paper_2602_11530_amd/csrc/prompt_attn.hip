@@ -61,6 +61,41 @@ constexpr int prompt_groups(int D, int keys, bool alone) { return D == 64 ? 4 : 
 struct Tokens {
   int s, first, count, at;
 };
+// The sum over the 64 lanes, the same for all: prefix sums of 16 lanes, then their last ones to the rows behind.
+__device__ __forceinline__ int sum_of_lanes(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);   // row_bcast 15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);   // row_bcast 31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+// The x-th group of `per` tokens, those first whose tokens see most keys, of up to 64 requests: a lane has one.  A request's groups see `per` keys more each,
+// so that it has one at each of some levels in a row, and those at or above a level are counted without a list of them.
+__device__ __forceinline__ Tokens tokens_in_order(const PromptLaunch& a, int x, int per) {
+  const int lane = threadIdx.x & 63, j = min(lane, a.S - 1);
+  const int begin = min(max(a.token_starts[j], 0), a.T), end = min(max(a.token_starts[j + 1], 0), a.T);
+  const int length = min(max(a.context_lens[j], 0), a.max_ctx);
+  const int n = lane < a.S ? max(end - begin, 0) : 0;
+  const int below = max(length - n, 0) / per, count = (n + per - 1) / per;     // its levels are below + 1 to below + count
+  auto at_or_above = [&](int level) { return sum_of_lanes(min(max(below + count + 1 - level, 0), count)); };
+  if (x >= sum_of_lanes(count)) return {0, 0, 0, 0};
+  int level = 0, more = 0;        // the highest with more than x groups at or above it
+  for (int step = 1 << (31 - __builtin_clz(a.max_ctx / per + a.T / per + 2)); step > 0; step >>= 1) {
+    const int c = at_or_above(level + step);
+    if (c > x) level += step;
+    else more = c;
+  }
+  const bool has = below < level && level <= below + count;
+  const uint64_t those = __ballot(has);
+  const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0));
+  const int s = __builtin_ctzll(__ballot(has && rank == x - more));
+  const int from = __builtin_amdgcn_readlane(begin, s), tokens = __builtin_amdgcn_readlane(n, s), L = __builtin_amdgcn_readlane(length, s);
+  const int slot = level - 1 - __builtin_amdgcn_readlane(below, s);
+  const int lo = max(slot * per, max(tokens - L, 0)), hi = min((slot + 1) * per, tokens);
+  return {s, from + lo, max(hi - lo, 0), L - tokens + lo};
+}
 // Slots of `per` tokens: request s has slots start / per + s and on, one or none of them empty.
 __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int per) {
   int s, from, end, L;
@@ -155,7 +190,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
   const int n = lane & 31, h = lane >> 5;
   const int kvh = blockIdx.x % a.Hkv;
   const int slot = slots - 1 - (int)(blockIdx.x / a.Hkv);        // late tokens see most: they begin first
-  const Tokens tok = tokens_of(a, slot, per);
+  const Tokens tok = !kAlone && a.ordered ? tokens_in_order(a, slots - 1 - slot, per) : tokens_of(a, slot, per);
   const int keys = tok.at + tok.count;                           // that the last one sees
   const int tiles = (keys + kKeyTile - 1) / kKeyTile;
   const int from = blockIdx.y * a.piece, to = min(from + a.piece, tiles);
@@ -659,6 +694,11 @@ PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
       p.pieces = (int)((tiles + piece - 1) / piece);
     }
   }
+  // The longest work first, else it ends alone: 24 pieces of 1..900 tokens behind 0..4096, 3 turns of the card, 254 -> 220 us, at D = 128 413 -> 383;
+  // sixteen prompts, 7 turns, 307 -> 301.  Not where all run at once (8.7 -> 9.0) nor in many turns, where a request's groups in a row share its keys in
+  // the caches (40 prompts, 18 turns, 720 -> 749).
+  const int64_t places = 256 * prompt_groups(D, prompt_keys(D, false), false);
+  p.ordered = !p.alone && p.pieces == 1 && S > 1 && S <= 64 && groups > places && groups <= 8 * places;
   if (p.pieces == 1) p.piece = max_ctx / (p.alone ? 32 : prompt_keys(D, false)) + 1;
   return p;
 }

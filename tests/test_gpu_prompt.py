@@ -400,3 +400,31 @@ def test_few_rows_are_those_of_many(kind):
     b.q_bits = np.concatenate([b.q_bits, wl.normal_bf16(b.rng, (500, 8, 128))])
     many = wl.bf16_bits_to_f64(run_prompt(b, p)).reshape(b.q_bits.shape)[:5]
     assert (np.abs(few - want) <= off).all() and (np.abs(many - want) <= off).all() and has.all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,hkv,dim,new", [(40, 20, 128, 200), (16, 8, 256, 500), (24, 24, 64, 330)])
+def test_longest_work_first(kind, hq, hkv, dim, new):
+    """More workgroups than run at once: requests of all lengths, some without tokens, one with more tokens than positions; rows of picked requests."""
+    rng = np.random.default_rng(hq)
+    many = rng.integers(1, new + 1, 30)
+    many[[4, 29]], many[11] = 0, 1
+    b = make_batch(rng.integers(0, 600, 30), many, hq, hkv, dim, 16, hq, lead=3, tail=70)
+    b.lens[7] = many[7] // 3
+    p = pools_of(b, kind)
+    got = run_prompt(b, p)
+    # the same bits in the order of the requests, as 65 of them are taken
+    few = b.lens, b.starts, b.tables
+    b.lens = np.r_[b.lens, np.zeros(35, np.int32)].astype(np.int32)
+    b.starts = np.r_[b.starts, np.full(35, b.starts[-1])].astype(np.int32)
+    b.tables = np.concatenate([b.tables, np.full((35, b.tables.shape[1]), -1, np.int32)])
+    assert np.array_equal(got, run_prompt(b, p))
+    b.lens, b.starts, b.tables = few
+    pick = [0, 7, 11, 23]
+    for s in pick:
+        one = make_batch([0], [int(many[s])], hq, hkv, dim, 16, 1)
+        one.lens, one.tables, one.num_blocks, one.scale = b.lens[s:s + 1], b.tables[s:s + 1], b.num_blocks, b.scale
+        rows = slice(int(b.starts[s]), int(b.starts[s + 1]))
+        one.q_bits = b.q_bits[rows]
+        check(one, got[rows], *plain_prompt(one, p))
+    assert (got[:3] == 0x7FC1).all() and (got[b.starts[-1]:] == 0x7FC1).all()
