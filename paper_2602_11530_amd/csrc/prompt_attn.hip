@@ -16,9 +16,9 @@
 //
 // Bound by the matrix unit and the vector unit together: 32 keys at D = 128 are 16 matrix instructions of 32 cycles and 90 vector ones, 16 of them
 // exponentials, in one chain, so that the wavefronts of a SIMD have to cover each other.  The matrix unit is busy for 63 % of one prompt of 8191 tokens
-// (40 heads on 8: 642 us, 1.07 PFLOP/s; a library product of 8192^3 reaches 1.21), for 45 % of sixteen of 100..2000 (300 us, 0.81), where a workgroup has
-// some ten tiles and its chain of four loads before the first (starts, table, unit, first product) is 3 us.
-//   128 rows: LDS is read once for 32 rows and memory once for 128; the LDS unit is active for 23 to 42 % of the time.  One wavefront with 64 rows
+// (40 heads on 8: 645 us, 1.06 PFLOP/s; a library product of 8192^3 reaches 1.21), for 45 % of sixteen of 100..2000 (303 us, 0.80), where a workgroup has
+// some twenty tiles and its chain of loads before the first (arguments, starts, table, unit) is 3 us.
+//   128 rows: LDS is read once for 32 rows and memory once for 128; the LDS unit is active for 23 to 45 % of the time.  One wavefront with 64 rows
 //   has no registers left at D = 128; eight wavefronts were no faster.
 //   Two tiles in LDS in turn, so that a tile's barrier is the only one.  Three: 664 -> 672 us.
 //   bf16 goes from memory straight into LDS, where each lane asks for the piece whose place is its own: no registers in between, no stores to LDS.
@@ -26,7 +26,7 @@
 //   LDS as it is, behind a second barrier (e4m3 203 -> 156 us, eight prompts of 200..1500 tokens).
 //   D = 256 in 256 registers, two workgroups to a unit, instead of one with 300: 194 -> 146 us.
 //   Few rows (kAlone): where a request has rows for one wavefront, three would wait for it.  All four take them, each with every fourth tile, in LDS of its
-//   own without barriers, nontemporal as nobody else reads it, and join in the end.  4 tokens of each of 32 requests with 1000..8000 behind them, memory's
+//   own without barriers, nontemporal as nobody else reads it as a rule, and join in the end.  4 tokens of each of 32 requests with 1000..8000 behind them, memory's
 //   case (592 MB): 125 -> 114 us (5.2 TB/s), 11 of them by the loads' kind; over e4m3 85 -> 64, of 200 requests 713 -> 636 (6.0 TB/s) and 448 -> 338.
 #include "attn_partial.h"
 #include "pkv_kernels.h"
@@ -46,7 +46,6 @@ constexpr float kLeast = -3e38f;                  // a reference maximum before 
 constexpr float kTooLarge = 0x1p120f;              // a scale whose products with e4m3 values may not be finite
 constexpr int kRawBuffer = 0x00020000;
 constexpr int kMfma = 0x8, kDsRead = 0x100;       // kinds of instructions, for the scheduler
-
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kMaxPieces = 64;                    // of a context
@@ -694,11 +693,11 @@ PromptPlan prompt_plan(int64_t T, int S, int Hkv, int G, int D, int max_ctx) {
       p.pieces = (int)((tiles + piece - 1) / piece);
     }
   }
-  // The longest work first, else it ends alone: 24 pieces of 1..900 tokens behind 0..4096, 3 turns of the card, 254 -> 220 us, at D = 128 413 -> 383;
-  // sixteen prompts, 7 turns, 307 -> 301.  Not where all run at once (8.7 -> 9.0) nor in many turns, where a request's groups in a row share its keys in
-  // the caches (40 prompts, 18 turns, 720 -> 749).
+  // The longest work first, else it ends alone: 24 pieces of 1..900 tokens behind 0..4096, 3 turns of the card, 254 -> 220 us, at D = 128 413 -> 383, in 5
+  // turns ten prompts 202 -> 197.  Not where all run at once (8.7 -> 9.0) nor in many turns, where a request's groups in a row share its keys in the caches
+  // (sixteen prompts, 7 turns, 303 -> 307, 40 of them, 18 turns, 720 -> 749).
   const int64_t places = 256 * prompt_groups(D, prompt_keys(D, false), false);
-  p.ordered = !p.alone && p.pieces == 1 && S > 1 && S <= 64 && groups > places && groups <= 8 * places;
+  p.ordered = !p.alone && p.pieces == 1 && S > 1 && S <= 64 && groups > places && groups <= 6 * places;
   if (p.pieces == 1) p.piece = max_ctx / (p.alone ? 32 : prompt_keys(D, false)) + 1;
   return p;
 }
