@@ -26,8 +26,9 @@
 //   LDS as it is, behind a second barrier (e4m3 203 -> 156 us, eight prompts of 200..1500 tokens).
 //   D = 256 in 256 registers, two workgroups to a unit, instead of one with 300: 194 -> 146 us.
 //   Few rows (kAlone): where a request has rows for one wavefront, three would wait for it.  All four take them, each with every fourth tile, in LDS of its
-//   own without barriers, nontemporal as nobody else reads it as a rule, and join in the end.  4 tokens of each of 32 requests with 1000..8000 behind them, memory's
+//   own without barriers, nontemporal where nobody else reads it, and join in the end.  4 tokens of each of 32 requests with 1000..8000 behind them, memory's
 //   case (592 MB): 125 -> 114 us (5.2 TB/s), 11 of them by the loads' kind; over e4m3 85 -> 64, of 200 requests 713 -> 636 (6.0 TB/s) and 448 -> 338.
+//   Of a request with more rows the loads are ordinary: 255 single tokens beside 1200 behind 4000 1074 -> 901 us, with 128 rows to a workgroup 912.
 #include "attn_partial.h"
 #include "pkv_kernels.h"
 
@@ -59,6 +60,7 @@ constexpr int prompt_groups(int D, int keys, bool alone) { return D == 64 ? 4 : 
 // A workgroup's tokens: `first` to `first + count` of the call, of request s, at position `at` and on.
 struct Tokens {
   int s, first, count, at;
+  bool only;   // the request's only ones
 };
 // The sum over the 64 lanes, the same for all: prefix sums of 16 lanes, then their last ones to the rows behind.
 __device__ __forceinline__ int sum_of_lanes(int x) {
@@ -79,7 +81,7 @@ __device__ __forceinline__ Tokens tokens_in_order(const PromptLaunch& a, int x, 
   const int n = lane < a.S ? max(end - begin, 0) : 0;
   const int below = max(length - n, 0) / per, count = (n + per - 1) / per;     // its levels are below + 1 to below + count
   auto at_or_above = [&](int level) { return sum_of_lanes(min(max(below + count + 1 - level, 0), count)); };
-  if (x >= sum_of_lanes(count)) return {0, 0, 0, 0};
+  if (x >= sum_of_lanes(count)) return {0, 0, 0, 0, true};
   int level = 0, more = 0;        // the highest with more than x groups at or above it
   for (int step = 1 << (31 - __builtin_clz(a.max_ctx / per + a.T / per + 2)); step > 0; step >>= 1) {
     const int c = at_or_above(level + step);
@@ -93,7 +95,7 @@ __device__ __forceinline__ Tokens tokens_in_order(const PromptLaunch& a, int x, 
   const int from = __builtin_amdgcn_readlane(begin, s), tokens = __builtin_amdgcn_readlane(n, s), L = __builtin_amdgcn_readlane(length, s);
   const int slot = level - 1 - __builtin_amdgcn_readlane(below, s);
   const int lo = max(slot * per, max(tokens - L, 0)), hi = min((slot + 1) * per, tokens);
-  return {s, from + lo, max(hi - lo, 0), L - tokens + lo};
+  return {s, from + lo, max(hi - lo, 0), L - tokens + lo, tokens <= per};
 }
 // Slots of `per` tokens: request s has slots start / per + s and on, one or none of them empty.
 __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int per) {
@@ -101,7 +103,7 @@ __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int
   if (!a.token_starts) {
     s = from = slot;
     end = from + 1;
-    if (s >= a.S) return {0, 0, 0, 0};
+    if (s >= a.S) return {0, 0, 0, 0, true};
     slot = 0;
     L = *(ScalarLoad)(a.context_lens + s);
   } else {
@@ -116,7 +118,7 @@ __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int
     const int j = base + lane, at = start(j);
     const int length = j < a.S ? a.context_lens[j] : 0;          // with the starts: one round trip less
     const int found = __popcll(__ballot(j < a.S && lane < 63 && at / per + j <= slot)) - 1;
-    if (found < 0) return {0, 0, 0, 0};
+    if (found < 0) return {0, 0, 0, 0, true};
     s = base + found;
     from = __builtin_amdgcn_readlane(at, found);
     end = __builtin_amdgcn_readlane(at, found + 1);
@@ -128,7 +130,7 @@ __device__ __forceinline__ Tokens tokens_of(const PromptLaunch& a, int slot, int
   // tokens before position 0 have none
   const int skip = max(n - L, 0);
   const int lo = max(slot * per, skip), hi = min((slot + 1) * per, n);
-  return {s, from + lo, max(hi - lo, 0), L - n + lo};
+  return {s, from + lo, max(hi - lo, 0), L - n + lo, n <= per};
 }
 
 __device__ __forceinline__ u32x2 widen(uint32_t w, float scale) {
@@ -138,14 +140,10 @@ __device__ __forceinline__ u32x2 widen(uint32_t w, float scale) {
 
 // 64 lanes' pieces of a buffer, zeros out of its bounds, to 1 KiB in a row of LDS from `to` on.  An opaque instruction: the compiler would wait for it
 // before every read of LDS that follows, whatever it reads.  Who asks waits for what was asked for, and meets the others, before anyone reads it.
-// kOnce: nobody else reads it, and it need not stay in the caches.
-template <bool kOnce>
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t b, uint32_t to, int offset) {
-  if constexpr (kOnce) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
-    return;
-  }
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
+// once: nobody else reads it, and it need not stay in the caches.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t b, uint32_t to, int offset, bool once) {
+  if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(b) : "memory");
 }
 
 // Places in LDS, in bytes: 16-byte piece p of key t.  K is read 16 bytes a lane, a key to a lane; V 8 bytes a lane, four keys of 64 bytes to half
@@ -297,25 +295,30 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
       int k0 = k_from, v0 = v_from;
       again(k0);
       again(v0);
+      auto loads = [&](auto kind) __attribute__((always_inline)) {
+        constexpr bool once = decltype(kind)::value;
 #pragma unroll
-      for (int y = 0; y < kEach; ++y) {
-        const int i = x * kEach + y;
-        if constexpr (kDirect) {
-          constexpr int kTokens = 64 / kPerToken;   // of a load
-          const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * 64 * ((kAlone ? 0 : wave * kLoads) + i);
-          load_to_lds<kAlone>(kb, to_lds, (k0 ^ k_place<kD>(kTokens * y, 0) % (kD * 2)) + kTokens * y * kD * kElem);
-          load_to_lds<kAlone>(vb, to_lds + kTileBytes, (v0 ^ v_place<kD>(kTokens * y, 0) % (kD * 2)) + kTokens * y * kD * kElem);
-        } else if constexpr (kStaged) {
-          const uint32_t to_lds = lds_at + 2 * kTileBytes + 16 * 64 * (wave * kLoads + i);
-          const int offset = 16 * (piece_of(i) % kOfUnit);
-          load_to_lds<kAlone>(kb, to_lds, offset);
-          load_to_lds<kAlone>(vb, to_lds + 16 * kSource, offset);
-        } else {
-          const int offset = 16 * (piece_of(i) % kOfUnit);
-          kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, kAlone ? 2 : 0));
-          vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, kAlone ? 2 : 0));
+        for (int y = 0; y < kEach; ++y) {
+          const int i = x * kEach + y;
+          if constexpr (kDirect) {
+            constexpr int kTokens = 64 / kPerToken;   // of a load
+            const uint32_t to_lds = lds_at + 2 * at_place * kTileBytes + 16 * 64 * ((kAlone ? 0 : wave * kLoads) + i);
+            load_to_lds(kb, to_lds, (k0 ^ k_place<kD>(kTokens * y, 0) % (kD * 2)) + kTokens * y * kD * kElem, once);
+            load_to_lds(vb, to_lds + kTileBytes, (v0 ^ v_place<kD>(kTokens * y, 0) % (kD * 2)) + kTokens * y * kD * kElem, once);
+          } else if constexpr (kStaged) {
+            const uint32_t to_lds = lds_at + 2 * kTileBytes + 16 * 64 * (wave * kLoads + i);
+            const int offset = 16 * (piece_of(i) % kOfUnit);
+            load_to_lds(kb, to_lds, offset, false);
+            load_to_lds(vb, to_lds + 16 * kSource, offset, false);
+          } else {
+            const int offset = 16 * (piece_of(i) % kOfUnit);
+            kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kb, offset, 0, once ? 2 : 0));
+            vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vb, offset, 0, once ? 2 : 0));
+          }
         }
-      }
+      };
+      if (kAlone && tok.only) loads(std::true_type{});
+      else loads(std::false_type{});
     }
   };
   // What is not finite in V of keys that some row may not see does not go through the matrix product, where a weight of zero does not silence it: it
