@@ -17,10 +17,6 @@
 namespace pkv {
 namespace {
 
-// The part of a request's new tokens that falls into one block: positions [from, to) of request s, `token` being the first one's.
-struct InBlock {
-  int s, from, to, token;
-};
 // Slots: request s has slots token_starts[s] / B + 2 * s and on, which are enough wherever its tokens begin in a block.  For all lanes the same.
 __device__ __forceinline__ InBlock in_block(const RopeLaunch& a, int slot) {
   typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
@@ -42,12 +38,7 @@ __device__ __forceinline__ InBlock in_block(const RopeLaunch& a, int slot) {
     end = __builtin_amdgcn_readlane(at, found + 1);
     k = slot - (start >> a.log_block) - 2 * s;
   }
-  const int L = min(max(*(ScalarLoad)(a.context_lens + s), 0), a.max_ctx), n = end - start;
-  if (n <= 0) return {0, 0, 0, 0};
-  const int first = max(L - n, 0);   // tokens before position 0 have none
-  const int block = (first >> a.log_block) + k;
-  const int from = max(first, block << a.log_block), to = min(L, (block + 1) << a.log_block);
-  return {s, from, to, end - (L - from)};
+  return tokens_in_block(s, start, end, min(max(*(ScalarLoad)(a.context_lens + s), 0), a.max_ctx), k, a.log_block);
 }
 
 __device__ __forceinline__ int pack_e4m3(float w, float x, float y, float z) {

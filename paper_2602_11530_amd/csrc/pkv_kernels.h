@@ -406,6 +406,22 @@ struct RopeLaunch {
 hipError_t launch_kv_rope(const RopeLaunch& a, hipStream_t stream);
 // The same into e4m3 pools with a scale for each block and KV head; q_out nullptr: no queries (kv_append_blk.hip).
 hipError_t launch_kv_append_blk(const RopeLaunch& a, uint8_t* k_scales, uint8_t* v_scales, hipStream_t stream);
+// The new tokens of request s that fall into one block: positions [from, to), `token` being the first one's.
+struct InBlock {
+  int s, from, to, token;
+};
+// Those of tokens [start, end), the last ones of a context of `length`, in the k-th block from the first one that they are in: none where from == to.
+// k counts on behind a request's last block, by as much as T / B where padding follows.
+__host__ __device__ inline InBlock tokens_in_block(int s, int start, int end, int length, int k, int log_block) {
+  const int n = end - start;
+  if (n <= 0) return {0, 0, 0, 0};
+  const int first = length > n ? length - n : 0;   // tokens before position 0 have none
+  const int block = (first >> log_block) + k;
+  if (block > (length - 1) >> log_block) return {0, 0, 0, 0};   // in blocks: the end of one behind the last may be past 2^31
+  const int begin = block << log_block, end_of_block = begin + (1 << log_block);
+  const int from = first > begin ? first : begin, to = length < end_of_block ? length : end_of_block;
+  return {s, from, to, end - (length - from)};
+}
 
 // Prompts: causal attention of new tokens over the paged cache (prompt_attn.hip).
 struct PromptLaunch {
