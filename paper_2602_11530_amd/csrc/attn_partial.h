@@ -25,26 +25,30 @@ struct Partial {
   f32x4 x;
 };
 constexpr Partial kNothing = {kNegInf, 0.f, {0.f, 0.f, 0.f, 0.f}};
+constexpr f32x2 kNoStats = {kNegInf, 0.f};   // of a result that is not there
 
 // Folds kN partial results into p: one common maximum first, so that the weights do not wait for
-// each other.  A side whose maximum is -inf (nothing valid seen) gets weight 0, and a weight of
-// exactly zero also silences whatever its row holds.
+// each other.  A side whose sum is exactly zero has seen nothing and is left out, whatever its row holds.  Every other one
+// counts, also with a weight of zero: one whose scores were all NaN has a sum of NaN and no maximum, and a NaN among values
+// that weigh nothing makes a NaN of the whole.
 template <int kN>
 __device__ __forceinline__ void fold(Partial& p, const f32x2 (&ml)[kN], const f32x4 (&x)[kN]) {
   float M = p.m;
 #pragma unroll
   for (int z = 0; z < kN; ++z) M = fmaxf(M, ml[z].x);
-  const float w = (p.m == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(p.m - M);
+  const float w = __builtin_amdgcn_exp2f(p.m - M);   // NaN where both are -inf: then the sum is zero or NaN
+  const bool some = p.l != 0.f;
   p.m = M;
-  p.l = (w != 0.f) ? w * p.l : 0.f;
+  p.l = some ? w * p.l : 0.f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) p.x[e] = (w != 0.f) ? w * p.x[e] : 0.f;
+  for (int e = 0; e < 4; ++e) p.x[e] = some ? w * p.x[e] : 0.f;
 #pragma unroll
   for (int z = 0; z < kN; ++z) {
-    const float wz = (ml[z].x == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(ml[z].x - M);
-    p.l = (wz != 0.f) ? __builtin_fmaf(wz, ml[z].y, p.l) : p.l;
+    const float wz = __builtin_amdgcn_exp2f(ml[z].x - M);
+    const bool there = ml[z].y != 0.f;
+    p.l = there ? __builtin_fmaf(wz, ml[z].y, p.l) : p.l;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) p.x[e] = (wz != 0.f) ? __builtin_fmaf(wz, x[z][e], p.x[e]) : p.x[e];
+    for (int e = 0; e < 4; ++e) p.x[e] = there ? __builtin_fmaf(wz, x[z][e], p.x[e]) : p.x[e];
   }
 }
 // Normalise, scale and round once to bf16.

@@ -46,7 +46,7 @@ struct SegmentRecords {
     }
 #pragma unroll
     for (int z = 0; z < kN; ++z) {
-      if (i + z * step >= count) ml[z].x = kNegInf;
+      if (i + z * step >= count) ml[z] = kNoStats;
     }
     fold(p, ml, x);
   }
@@ -103,7 +103,7 @@ __device__ __forceinline__ void reduce_segment(const AttnLaunch& a, const Layers
         const int t = threadIdx.x + (there ? (z + 1) * left * mine * 16 : 0);
         x[z] = rows[t];
         ml[z] = stats[t];
-        if (!there) ml[z].x = kNegInf;
+        if (!there) ml[z] = kNoStats;
       }
       fold(p, ml, x);
     }

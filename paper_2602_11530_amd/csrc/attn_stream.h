@@ -1263,7 +1263,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       }
 #pragma unroll
       for (int z = 0; z < kAtOnce; z += 2) {   // two by two, so that every way here gives the same bits
-        const f32x2 ml2[2] = {k + z > v ? f32x2{kNegInf, 0.f} : ml[z], k + z + 1 > v ? f32x2{kNegInf, 0.f} : ml[z + 1]};
+        const f32x2 ml2[2] = {k + z > v ? kNoStats : ml[z], k + z + 1 > v ? kNoStats : ml[z + 1]};
         const f32x4 x2[2] = {x[z], x[z + 1]};
         fold(p, ml2, x2);
       }

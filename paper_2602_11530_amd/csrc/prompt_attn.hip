@@ -597,7 +597,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(f32x4*)(part + 32 * d + 8 * g + 4 * half) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
-    if (half == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + row.of_call) * 2) = f32x2{m == kLeast ? kNegInf : m, total};
+    if (half == 0) *(f32x2*)(a.stats + ((int64_t)blockIdx.y * a.T * a.Hq + row.of_call) * 2) = f32x2{m, total};
   }
 }
 
@@ -639,7 +639,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
       }
 #pragma unroll
       for (int z = 0; z < kAtOnce; ++z)
-        if (i + z >= count) ml[z] = f32x2{kNegInf, 0.f};
+        if (i + z >= count) ml[z] = kNoStats;
       fold(p, ml, x);
     }
     *(u32x2*)(a.out + row * kD + dim) = finish_row4(p.x, inverse(p.l, a.out_scale));
