@@ -106,7 +106,8 @@ int pkv_attn_workspace_bytes(const pkv_attn_shape* shape /* host */, size_t* out
  * arithmetic and stays where it belongs: a NaN in a K row turns the rows of
  * that KV head's query group into NaN, a NaN V element turns that output
  * element into NaN, an infinite V element leaves it non-finite (NaN or Inf);
- * every other output element is unaffected.
+ * every other output element is unaffected.  A token whose score is minus infinity
+ * (an infinite K element) weighs nothing; a row that sees no other is NaN.
  *
  * Arithmetic: bf16 inputs, fp32 scores, softmax statistics and accumulation,
  * one round-to-nearest-even to bf16 at the end.  The result does not depend on

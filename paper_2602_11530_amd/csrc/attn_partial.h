@@ -13,6 +13,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNegInf = -__builtin_huge_valf();
+// A reference maximum before any score.  Finite, so that weights of minus infinity are zeros, those of what is masked and those of infinite keys; a result
+// that has seen tokens keeps at least this, one that has not has minus infinity.
+constexpr float kLeast = -3e38f;
 
 // Two fp32 -> packed bf16, round to nearest even (v_cvt_pk_bf16_f32).
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -55,8 +58,10 @@ __device__ __forceinline__ void fold(Partial& p, const f32x2 (&ml)[kN], const f3
 __device__ __forceinline__ u32x2 finish_row4(f32x4 x, float inv) {
   return u32x2{pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv)};
 }
-__device__ __forceinline__ float inverse(float l, float out_scale) {
-  return l > 0.f ? out_scale / l : 0.f;
+// Zeros where nothing was seen.  Where none of the tokens that were seen has a weight, the row of zeros is multiplied by infinity, which is NaN: the quotient
+// of two zeros.
+__device__ __forceinline__ float inverse(float m, float l, float out_scale) {
+  return m > kNegInf ? out_scale / l : 0.f;
 }
 
 }  // namespace pkv

@@ -65,7 +65,7 @@ __device__ __forceinline__ void reduce_segment(const AttnLaunch& a, const Layers
     r.stats = 4 * a.G * kD + 8 * (chunk / kHeadChunks);
   };
   auto finish = [&](const Partial& p, int chunk) {
-    *(u32x2*)(out + 64 * chunk + 4 * lane16) = finish_row4(p.x, inverse(p.l, a.out_scale));
+    *(u32x2*)(out + 64 * chunk + 4 * lane16) = finish_row4(p.x, inverse(p.m, p.l, a.out_scale));
   };
   if (count <= 2 * kBatch) {
     if (slice != 0 || sub >= chunks) return;

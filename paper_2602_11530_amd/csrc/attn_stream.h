@@ -615,7 +615,8 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
   const int voff = kD == 256 ? 32 * c + n : lane;
 
   u32x4 qop[kKSteps];  // q as the B operand: dims 32*jj + 8*c .. +7 of head n; zero rows beyond the group
-  float m = kNegInf;   // running reference maximum of head n (log2 units), same in all four c groups
+  float m = kLeast;    // running reference maximum of head n (log2 units), same in all four c groups
+  int counted = 0;     // not zero once a token of the run counts
   float l = 0.f;       // this lane's share of the softmax denominator
   f32x4 o[kTiles];     // o[i][r]: head 4*c + r, dim tile_group_dim(i / 4, n) + i % 4
 #pragma unroll
@@ -749,6 +750,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
         }
       }
       next.k(kraw);
+      counted |= (int)seen;
       const bool edge = seen != 0xffffffffu;
       const uint32_t mine = seen >> (4 * c);
       auto valid = [&](int i) { return (mine >> (16 * (i >> 2) + (i & 3))) & 1; };   // token 4*c + i % 4 of tile i / 4
@@ -795,7 +797,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       if (__any(mx > m + kLazyLog2)) {
         float mg = fmaxf(mx, __shfl_xor(mx, 16));
         mg = fmaxf(mg, __shfl_xor(mg, 32));
-        const float mnew = fmaxf(m, mg);   // finite: some lane of the head saw a valid token
+        const float mnew = fmaxf(m, mg);
         const float alpha = __builtin_amdgcn_exp2f(m - mnew);
         l *= alpha;
         float ar[4];
@@ -812,7 +814,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       for (int i = 0; i < 8; ++i) pw[i] = __builtin_amdgcn_exp2f(x[i] - m);
       if (edge) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pw[i] = valid(i) ? pw[i] : 0.f;   // m may still be -inf here
+        for (int i = 0; i < 8; ++i) pw[i] = valid(i) ? pw[i] : 0.f;   // of a score of NaN, too
       }
       l += ((pw[0] + pw[1]) + (pw[2] + pw[3])) + ((pw[4] + pw[5]) + (pw[6] + pw[7]));
       u32x4 hi, lo;   // P = hi + lo in bf16
@@ -874,6 +876,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       }
       const int ntok = meta & 0xff;
       const uint32_t seen = (uint32_t)meta >> 16;   // with a span
+      counted |= kSpan ? (int)seen : ntok;
 
       f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -903,7 +906,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       if (__any(mx > m + kLazyLog2)) {
         float mg = fmaxf(mx, __shfl_xor(mx, 16));
         mg = fmaxf(mg, __shfl_xor(mg, 32));
-        const float mnew = fmaxf(m, mg);   // finite: some lane of the head saw a valid token
+        const float mnew = fmaxf(m, mg);
         const float alpha = __builtin_amdgcn_exp2f(m - mnew);
         l *= alpha;
         float ar[4];
@@ -920,7 +923,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       for (int e = 0; e < 4; ++e) pw[e] = __builtin_amdgcn_exp2f(x[e] - m);
       if (edge) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pw[e] = valid[e] ? pw[e] : 0.f;   // m may still be -inf here
+        for (int e = 0; e < 4; ++e) pw[e] = valid[e] ? pw[e] : 0.f;
       }
       l += (pw[0] + pw[1]) + (pw[2] + pw[3]);
 
@@ -960,6 +963,8 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       float* rec = open_left ? rec_left : rec_right;
       float lt = l + __shfl_xor(l, 16);
       lt += __shfl_xor(lt, 32);
+      if (!counted) m = kNegInf;
+      counted = 0;
       if (seg_open) {
         // parked (m1, l1, rows1) and this run's (m, lt, o): weights 2^(m1-M) and 2^(m-M),
         // a side whose maximum is -inf (nothing valid seen) gets weight 0 by select
@@ -986,7 +991,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
         if (nstaged == a.staged_max) store_staged();
         staged_segs = (lane == nstaged) ? seg : staged_segs;
         uint16_t* rows = staged + nstaged * G * kD;
-        const float inv = inverse(lt, a.out_scale);
+        const float inv = inverse(m, lt, a.out_scale);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int h = 4 * c + r;
@@ -1019,7 +1024,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
         if (c == 0) *(f32x2*)(rec + G * kD + 2 * n) = (n < G) ? f32x2{m, lt} : f32x2{kNegInf, 0.f};
       }
       seg_open = true;
-      m = kNegInf;
+      m = kLeast;
       l = 0.f;
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1269,7 +1274,7 @@ __global__ __launch_bounds__(group_waves(kD) * 64) void attn_stream_kernel(AttnL
       }
     }
     if (kWhole || (from_right && !open_right)) {
-      *(u32x2*)(out + (int64_t)(kWhole ? seg_next : left_seg[v]) * (G * kD) + 4 * item) = finish_row4(p.x, inverse(p.l, out_scale));
+      *(u32x2*)(out + (int64_t)(kWhole ? seg_next : left_seg[v]) * (G * kD) + 4 * item) = finish_row4(p.x, inverse(p.m, p.l, out_scale));
     } else {
       float* rec = group_record(b, kD, of, blockIdx.x, from_right);
       store16(rec + 4 * item, __builtin_bit_cast(u32x4, p.x));

@@ -43,7 +43,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef const int32_t __attribute__((address_space(4))) * ScalarLoad;
 
 constexpr float kLazyLog2 = 8.f;
-constexpr float kLeast = -3e38f;                  // a reference maximum before any score: finite, so that what is masked, -inf, gives weights of zero
 constexpr float kTooLarge = 0x1p120f;              // a scale whose products with e4m3 values may not be finite
 constexpr int kRawBuffer = 0x00020000;
 constexpr int kMfma = 0x8, kDsRead = 0x100;       // kinds of instructions, for the scheduler
@@ -582,8 +581,14 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
   }
   const float total = kAlone ? l : l + __shfl_xor(l, 32);
   const int64_t q_row = (int64_t)row.of_call * kD;
+  if (__builtin_expect(__any(total == 0.f), 0)) {   // these rows have seen nothing, or nothing that weighs anything
+    const ScalarLoad ids = (ScalarLoad)(a.block_tables + (int64_t)tok.s * a.MAXB);
+    int key = from * kKeyTile;                      // the first of a block that is there
+    while (key < min(context, to * kKeyTile) && (unsigned)ids[key >> a.log_block] >= (unsigned)a.NB) key = ((key >> a.log_block) + 1) << a.log_block;
+    if (key >= to * kKeyTile || key > row.last_key) m = kNegInf;
+  }
   if (tiles <= a.piece) {
-    const float inv = inverse(total, a.out_scale);
+    const float inv = inverse(m, total, a.out_scale);
 #pragma unroll
     for (int d = 0; d < kTiles; ++d)
 #pragma unroll
@@ -642,7 +647,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptLaunch a, int pe
         if (i + z >= count) ml[z] = kNoStats;
       fold(p, ml, x);
     }
-    *(u32x2*)(a.out + row * kD + dim) = finish_row4(p.x, inverse(p.l, a.out_scale));
+    *(u32x2*)(a.out + row * kD + dim) = finish_row4(p.x, inverse(p.m, p.l, a.out_scale));
   }
 }
 
