@@ -215,7 +215,8 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
 
   bf16x8 q[kSteps];
   const bool negative = a.scale_log2e < 0.f;
-  const float scale = fmaxf(__builtin_fabsf(a.scale_log2e), 0x1p-126f);   // masked scores stay -inf with a scale of zero, too
+  // masked scores stay -inf with a scale of zero, too; NaN stays NaN
+  const float scale = __builtin_fabsf(a.scale_log2e) < 0x1p-126f ? 0x1p-126f : __builtin_fabsf(a.scale_log2e);
 #pragma unroll
   for (int jj = 0; jj < kSteps; ++jj) {
     u32x4 x = *(const u32x4*)(a.q + (int64_t)row_of(lane).of_call * kD + 16 * jj + 8 * h);
