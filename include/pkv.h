@@ -555,7 +555,9 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
  * request's last token are never read.
  *
  * bf16 inputs, fp32 scores, softmax statistics and accumulation; a weight is rounded to bf16
- * before it multiplies V (relative error 2^-8), and a row once, to bf16, at the end.  No bit of a row depends on where
+ * before it multiplies V (relative error 2^-8; over bf16 pools and where num_tokens is at most num_seqs times
+ * the tokens that have 32 rows, 32 / (Hq / Hkv) rounded down, to two bf16 numbers as in paged_decode_attn, 2^-16),
+ * and a row once, to bf16, at the end.  No bit of a row depends on where
  * its blocks are nor on the other requests' contents, but its last bits depend on T, num_seqs and
  * max_context_len, which choose how contexts are cut.
  *

@@ -11,8 +11,10 @@
 //   O^T  += V^T . P^T  D/32 times two for 32 keys.  P is the B operand as it came out; A takes dims in rows out of V's rows of dims by
 //         transposing reads of LDS, four keys of 16 dims to 16 lanes, in the order of keys that P has.
 // The running maximum is only raised when a score exceeds it by more than 2^8, as in the decode kernels.  A weight is one bf16 number here, off by
-// 2^-8 of itself at most, while the decode kernels take two: the second would cost half as many matrix instructions again, and many weights make up a
-// row, so that rows are 0.0021 from those in 64 bits (relative L2) where the rounding of the output alone makes 0.0016.
+// 2^-8 of itself at most, while the decode kernels take two: the second is half as many matrix instructions again (one prompt of 8191 tokens 635 -> 860 us,
+// sixteen of 100..2000 304 -> 385, at D = 256 130 -> 206), and many weights make up a row, so that rows are 0.0020 to 0.0023 from those in 64 bits (relative
+// L2) where the rounding of the output alone makes 0.0016.  Few rows (kAlone) over bf16 pools wait for memory and have both numbers (4 tokens of each of 32
+// requests 112.4 and 112.5 us), over 8-bit pools one (65 us, with two 71; at D = 64 67 and 75).
 //
 // Bound by the matrix unit and the vector unit together: 32 keys at D = 128 are 16 matrix instructions of 32 cycles and 90 vector ones, 16 of them
 // exponentials, in one chain, so that the wavefronts of a SIMD have to cover each other.  The matrix unit is busy for 63 % of one prompt of 8191 tokens
@@ -173,6 +175,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
   constexpr int kOwn = kAlone ? kUnits : 1, kEach = kLoads / kOwn;   // units that a wavefront loads from, its loads of one
   static_assert(kEach * kOwn * (kAlone ? 64 : kThreads) == kSource && kOfUnit % (64 * kEach) == 0, "whole units, or pieces of one");
   constexpr bool kDirect = kFormat == 0;                         // nothing to widen: from memory straight into LDS
+  constexpr bool kTwo = kAlone && kFormat == 0;                  // weights are two bf16 numbers
   constexpr bool kStaged = kFormat != 0 && kD == 256 && !kAlone;            // on its way to registers through LDS
   constexpr bool kHide = kD > 64 && kKeyTile == 32 && !kAlone;              // registers are short: what is cheap to find again is not kept in one over the loop
   constexpr int kReadsAhead = kAlone ? 4 : kD == 256 ? 2 : kKeyTile == 32 ? 3 : 6;   // of LDS in the first product, as many as there are registers for
@@ -453,7 +456,7 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
       m = raised;
     }
-    u32x4 p[2 * kHalves];   // weights of keys 16*step .. +15, the B operand
+    [[maybe_unused]] u32x4 p[2 * kHalves];   // weights of keys 16*step .. +15, the B operand
     float sum[kHalves] = {};
 #pragma unroll
     for (int b = 0; b < kHalves; ++b) {
@@ -462,17 +465,38 @@ __global__ __launch_bounds__(kThreads, prompt_groups(kD, kKeyTile, kAlone)) void
         s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], scale, -m));
         sum[b] += s[b][r];
       }
+      if constexpr (!kTwo)
 #pragma unroll
-      for (int z = 0; z < 8; ++z) p[2 * b + (z >> 2)][z & 3] = pack_bf16(s[b][2 * z], s[b][2 * z + 1]);
+        for (int z = 0; z < 8; ++z) p[2 * b + (z >> 2)][z & 3] = pack_bf16(s[b][2 * z], s[b][2 * z + 1]);
     }
     again(v_at);
     l += kHalves == 2 ? sum[0] + sum[kHalves - 1] : sum[0];
 #pragma unroll
-    for (int step = 0; step < 2 * kHalves; ++step)
+    for (int step = 0; step < 2 * kHalves; ++step) {
+      if constexpr (kTwo) {
+        // here, not with the exponentials, and the products of what the rounding left behind those of all dims: no more registers than one number takes
+        u32x4 high, low, v[kTiles];
 #pragma unroll
-      for (int d = 0; d < kTiles; ++d)
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v_lds, v_at, step, d)), __builtin_bit_cast(bf16x8, p[step]), o[d],
-                                                       0, 0, 0);
+        for (int z = 0; z < 4; ++z) {
+          const float x = s[step >> 1][8 * (step & 1) + 2 * z], y = s[step >> 1][8 * (step & 1) + 2 * z + 1];
+          high[z] = pack_bf16(x, y);
+          low[z] = pack_bf16(x - __uint_as_float(high[z] << 16), y - __uint_as_float(high[z] & 0xffff0000u));
+        }
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d) {
+          v[d] = v_operand(v_lds, v_at, step, d);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[d]), __builtin_bit_cast(bf16x8, high), o[d], 0, 0, 0);
+        }
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[d]), __builtin_bit_cast(bf16x8, low), o[d], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int d = 0; d < kTiles; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand(v_lds, v_at, step, d)), __builtin_bit_cast(bf16x8, p[step]),
+                                                         o[d], 0, 0, 0);
+      }
+    }
   };
 
   for (int d = threadIdx.x; d < kD; d += kThreads) first_bad[d] = INT32_MAX;
