@@ -246,7 +246,8 @@ int pkv_fp8blk_scale_bytes(const pkv_attn_shape* shape /* host */, size_t* out_b
  * paged_decode_attn over such pools (q and out bf16, fp32 arithmetic).  Byte and scale
  * are widened together to bf16, exactly for scale bytes of 10 to 246, the ones that the
  * appends write, so the result is the attention of the de-quantised pools to the same
- * tolerance as the bf16 call.  Scales of blocks that hold no token of a request are not
+ * tolerance as the bf16 call.  (Values of a block with a larger scale byte may count as not
+ * finite.)  Scales of blocks that hold no token of a request are not
  * used; unused slots and unused blocks may hold any bytes.
  *
  *   k_pool, v_pool      device  e4m3  [NB][Hkv][B][D]
@@ -551,7 +552,7 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
  * head (_fp8blk).  Rows of tokens without a position (see kv_rope_append; padding among
  * them) are left as they were.  Tokens of blocks whose id lies outside [0, num_pool_blocks)
  * are left out of the softmax; a row that sees no other is all zeros.  What is not finite in K or V of a token reaches the
- * rows that see it alone, as in paged_decode_attn.  Table entries and slots behind a
+ * rows that see it alone, as in paged_decode_attn: an infinite V element leaves that output element NaN or infinite.  Table entries and slots behind a
  * request's last token are never read.
  *
  * bf16 inputs, fp32 scores, softmax statistics and accumulation; a weight is rounded to bf16
@@ -559,11 +560,12 @@ int kv_rope_append_fp8blk(const void* q, const void* k, const void* v, const voi
  * the tokens that have 32 rows, 32 / (Hq / Hkv) rounded down, to two bf16 numbers as in paged_decode_attn, 2^-16),
  * and a row once, to bf16, at the end.  No bit of a row depends on where
  * its blocks are nor on the other requests' contents, but its last bits depend on T, num_seqs and
- * max_context_len, which choose how contexts are cut.
+ * max_context_len, which choose how contexts are cut.  The time depends on them, too: where tokens are few, contexts are cut as if all
+ * had max_context_len tokens, and with a bound four times the lengths and more such calls take 1.2 to 1.7 times as long.
  *
  *   q             device  bf16  [T][Hq][D], rows of tokens without gaps
  *   token_starts  device  int32 [num_seqs + 1], ascending, or NULL: one token for each request, T = num_seqs
- *   num_tokens    T, 0..2^24-1
+ *   num_tokens    T, 0..2^24-1, and T * Hq below 2^31 (2^29 where tokens are few for num_seqs) less what incomplete groups take (PKV_ERR_SHAPE)
  *   out           device  bf16  [T][Hq][D]; may be q itself, and must not overlap q otherwise, nor the
  *                 pools, scales or tables (PKV_ERR_SHAPE)
  *   shape         host    (partition_size is not used); max_context_len, or MAXB*B if that is 0, at most 2^31 - 4097

@@ -8,8 +8,10 @@
 // among them without leaving registers, and write: no workgroup waits for another, nothing is read twice.  A scale's byte is read by all lanes of the
 // group and written by one: where those are several wavefronts, behind the barrier at which they compare.
 //
-// Bound by memory: sixteen prompts of 100..2000 tokens on 40/8 heads (470 MB read and written) 90 us, 5.2 TB/s, 24 of them for K and V and 52 for the
-// queries in the trace; pieces at D = 64 in 64-token blocks 26 us, 4.0 TB/s.  A step is one chain of loads, 2.8 us for 4 requests and 4.8 for 64.
+// Bound by memory: sixteen prompts of 100..2000 tokens on 40/8 heads (470 MB read and written) 91 us, 5.2 TB/s, 26 of them for K and V and 53 for the
+// queries in the trace; pieces at D = 64 in 64-token blocks 27 us, 3.9 TB/s.  A step is one chain of loads, 2.8 us for 4 requests and 4.4 to 4.8 for 64
+// where no scale grows.  Where some do, the rows that such a block held follow one after the other: with normal values 35 of 1024 blocks and heads of 64
+// requests in 16-token blocks, and the step takes 8.6 us; 25 in 32-token blocks and 12.3; 16 in 64-token blocks and 19.3.
 //   Rows spread over groups of lanes, at most 8 to a lane, all 8 asked for at once: with one group for a block, which takes its rows one after the
 //   other and reads them twice, prompts took 102 us and pieces 59.
 #include "kv_rope.h"
